@@ -3,13 +3,15 @@ import os
 import subprocess
 import sys
 import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 LIB_PATH = os.path.join(HERE, "libsdp.so")
 SOURCES = [os.path.join(HERE, "csrc", f)
            for f in ("sdp_runtime.hip", "sdp_stream.hip", "sdp_host_route.hip", "sdp_kernels.hip",
-                     "sdp_copy.hip", "sdp_noalloc.hip")]
+                     "sdp_copy.hip", "sdp_noalloc.hip", "sdp_ops.hip", "sdp_qk.hip", "sdp_grouped.hip",
+                     "sdp_distill.hip")]
 # host-only lanes, built with the host compiler: no fused multiply-add, so the
 # FP64 update rounds every product and sum as written
 HOST_SOURCES = [os.path.join(HERE, "csrc", f) for f in ("sdp_host_adamw.cpp", "sdp_schedule.cpp")]
@@ -29,16 +31,20 @@ FLAGS = [
 def build(verbose: bool = False) -> str:
     tmp = LIB_PATH + ".tmp"
     inc = ["-I", os.path.join(ROOT, "include"), "-I", os.path.join(HERE, "csrc")]
+    # one compiler process for each source, up to the machine's CPUs (8 at most)
+    compile_flags = [f for f in FLAGS if f != "-shared"]
     with tempfile.TemporaryDirectory() as d:
-        objs = []
-        for src in HOST_SOURCES:
+        def compiled(src: str) -> str:
             obj = os.path.join(d, os.path.basename(src) + ".o")
-            cmd = [HOSTCXX, *HOST_FLAGS, *inc, "-c", src, "-o", obj]
+            tool = [HIPCC, *compile_flags] if src in SOURCES else [HOSTCXX, *HOST_FLAGS]
+            cmd = [*tool, *inc, "-c", src, "-o", obj]
             if verbose:
                 print(" ".join(cmd), flush=True)
             subprocess.check_call(cmd)
-            objs.append(obj)
-        cmd = [HIPCC, *FLAGS, *inc, "-o", tmp, *SOURCES, "-x", "none", *objs]
+            return obj
+        with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            objs = list(pool.map(compiled, SOURCES + HOST_SOURCES))
+        cmd = [HIPCC, *FLAGS, "-o", tmp, *objs]
         if verbose:
             print(" ".join(cmd), flush=True)
         subprocess.check_call(cmd)

@@ -1,0 +1,100 @@
+// Decisions of the training operators' host code that need no device, free of
+// HIP so that they can be checked without one: extents and overlaps of strided
+// tensors, and the multipliers that stand for divisions in the kernels.
+#pragma once
+
+#include <cstdint>
+
+namespace sdpops {
+
+// A strided tensor of up to three outer dimensions around `inner` contiguous
+// elements; strides count elements.
+struct Layout {
+    int64_t ext[3];
+    int64_t stride[3];
+    int64_t inner;
+};
+
+inline bool no_elements(const Layout &l) { return l.inner == 0 || l.ext[0] == 0 || l.ext[1] == 0 || l.ext[2] == 0; }
+
+// Elements from the first to the last one, or -1 where that does not fit 60
+// bits or a stride is negative.
+inline int64_t span(const Layout &l) {
+    if (no_elements(l)) return 0;
+    __int128 s = l.inner;
+    for (int k = 0; k < 3; ++k) {
+        if (l.stride[k] < 0) return -1;
+        s += (__int128)(l.ext[k] - 1) * l.stride[k];
+    }
+    return s < ((__int128)1 << 60) ? (int64_t)s : -1;
+}
+
+// Whether no two index tuples name the same element, by the sufficient test
+// that each dimension steps past all that the smaller ones cover.
+inline bool injective(const Layout &l) {
+    if (no_elements(l)) return true;
+    int order[3] = {0, 1, 2};
+    for (int i = 0; i < 3; ++i)
+        for (int j = i + 1; j < 3; ++j)
+            if (l.stride[order[j]] < l.stride[order[i]]) {
+                const int t = order[i];
+                order[i] = order[j];
+                order[j] = t;
+            }
+    __int128 covered = l.inner;
+    for (int k : order) {
+        if (l.ext[k] == 1) continue;
+        if ((__int128)l.stride[k] < covered) return false;
+        covered += (__int128)(l.ext[k] - 1) * l.stride[k];
+    }
+    return true;
+}
+
+// Whether the strides agree wherever both tensors step, so that equal
+// addresses mean the same tensor.
+inline bool same_strides(const Layout &a, const Layout &b) {
+    for (int k = 0; k < 3; ++k)
+        if (a.ext[k] > 1 && b.ext[k] > 1 && a.stride[k] != b.stride[k]) return false;
+    return true;
+}
+
+inline bool same_tensor(const char *pa, const Layout &a, const char *pb, const Layout &b) {
+    if (pa != pb || a.inner != b.inner) return false;
+    for (int k = 0; k < 3; ++k)
+        if (a.ext[k] != b.ext[k] || (a.ext[k] > 1 && a.stride[k] != b.stride[k])) return false;
+    return true;
+}
+
+// Whether two tensors of elements of `size` bytes share no element: their
+// byte ranges are apart, or they are runs of heads (dimension 2) of one fused
+// tensor, whose runs do not meet.  Where neither can be shown, false.
+inline bool disjoint(const char *pa, const Layout &a, const char *pb, const Layout &b, int64_t size) {
+    if (no_elements(a) || no_elements(b)) return true;
+    const int64_t sa = span(a) * size, sb = span(b) * size;
+    if (pa + sa <= pb || pb + sb <= pa) return true;
+    if (a.inner != b.inner || !same_strides(a, b)) return false;
+    const bool a_first = pa <= pb;
+    const Layout &lo = a_first ? a : b, &hi = a_first ? b : a;
+    const int64_t apart = a_first ? pb - pa : pa - pb;
+    const int64_t hs = lo.ext[2] > 1 ? lo.stride[2] : hi.ext[2] > 1 ? hi.stride[2] : lo.inner;
+    if (hs < lo.inner || apart % (hs * size) != 0) return false;
+    const int64_t first = apart / (hs * size);
+    if (first < lo.ext[2]) return false;
+    Layout all = lo;
+    for (int k = 0; k < 2; ++k) {
+        if (lo.ext[k] <= 1) all.stride[k] = hi.stride[k];
+        if (hi.ext[k] > all.ext[k]) all.ext[k] = hi.ext[k];
+    }
+    all.stride[2] = hs;
+    all.ext[2] = first + hi.ext[2];
+    return injective(all);
+}
+
+// n / d as (n * m) >> 32 with m = floor(2^32 / d) + 1: the product exceeds
+// n * 2^32 / d by n * e / d with 1 <= e <= d, which reaches the next whole
+// quotient only from n * e >= 2^32 on, so it is exact for n < 2^32 / d.
+// d = 1 would need a multiplier past 32 bits: 0 stands for it.
+inline uint32_t quotient_multiplier(uint32_t d) { return d <= 1 ? 0 : (uint32_t)((((uint64_t)1) << 32) / d + 1); }
+inline uint32_t quotient(uint32_t n, uint32_t m) { return m == 0 ? n : (uint32_t)(((uint64_t)n * m) >> 32); }
+
+}  // namespace sdpops

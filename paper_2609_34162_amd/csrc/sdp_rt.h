@@ -274,6 +274,11 @@ struct sdp_ctx {
     int64_t host_issues = 0;
     int64_t host_adam_elems = 0;
     std::vector<hipEvent_t> pool;
+    // training operators (sdp_ops.hip): their workspace, and the last call that used it
+    char *ops_space = nullptr;
+    size_t ops_space_cap = 0;
+    hipEvent_t ops_done = nullptr;
+    bool ops_done_valid = false;
 };
 
 namespace sdprt {

@@ -918,6 +918,8 @@ void sdp_ctx_destroy(sdp_ctx *ctx) {
     delete ctx->copier;
     if (ctx->partials) (void)hipFree(ctx->partials);
     if (ctx->gbar) (void)hipFree(ctx->gbar);
+    if (ctx->ops_space) (void)hipFree(ctx->ops_space);
+    if (ctx->ops_done) (void)hipEventDestroy(ctx->ops_done);
     if (ctx->ns) (void)hipFree(ctx->ns);
     if (ctx->ns_host) (void)hipHostFree(ctx->ns_host);
     (void)hipGetLastError();

@@ -1,0 +1,135 @@
+"""sdp_grouped_matmul and its backward on the GPU against 64-bit products."""
+import pytest
+
+import gpu_util
+import ops_ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    sdp = gpu_util.need_gpu()
+    c = sdp.sdp_ctx_create(0, 0, 1, 0)
+    yield c
+    torch.cuda.synchronize()
+    sdp.sdp_ctx_destroy(c)
+
+
+def strided(gen, rows, cols, pad, dtype=BF16, offset=0):
+    """[rows, cols], rows cols + pad apart, the first element `offset` past an aligned one; NaN between the rows."""
+    flat = torch.full((offset + rows * (cols + pad) + 8,), float("nan"), dtype=dtype)
+    t = flat.cuda()[offset:offset + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+    t.copy_(torch.randn((rows, cols), generator=gen))
+    return t
+
+
+def check_all(ctx, counts, n_in, n_out, unused=0, out=BF16, ends=torch.int32, pad=0, offset=0, seed=0, want_ends=None):
+    from paper_2609_34162_amd import ops
+    gen = torch.Generator().manual_seed(seed)
+    rows, groups = sum(counts) + unused, len(counts)
+    e = torch.tensor(counts, dtype=torch.int64).cumsum(0).to(ends).cuda() if want_ends is None else \
+        torch.tensor(want_ends, dtype=ends).cuda()
+    x, dy = strided(gen, rows, n_in, pad, offset=offset), strided(gen, rows, n_out, pad, offset=offset)
+    if unused:
+        # what lies in rows of no group is not used
+        x[rows - unused:] = float("inf")
+        dy[rows - unused:] = float("nan")
+    w = strided(gen, groups * n_out, n_in, 0, offset=offset).view(groups, n_out, n_in)
+    y = torch.full((rows, n_out + pad), 7.0, dtype=out, device="cuda")[:, :n_out]
+    dx = torch.full((rows, n_in + pad), 7.0, dtype=BF16, device="cuda")[:, :n_in]
+    dw = torch.full((groups, n_out, n_in), 7.0, dtype=out, device="cuda")
+    ops.sdp_grouped_matmul(ctx, x, w, e, y)
+    ops.sdp_grouped_matmul_backward(ctx, x, w, e, dy, dx, dw)
+    ops_ref.check(y, *ops_ref.grouped(x, w, e, out), "y")
+    (rx, bx), (rw, bw) = ops_ref.grouped_back(x, w, e, dy, out)
+    ops_ref.check(dx, rx, bx, "dx")
+    ops_ref.check(dw, rw, bw, "dw")
+    if pad:
+        assert (y.as_strided((rows, pad), (n_out + pad, 1), y.storage_offset() + n_out) == 7).all()
+        assert (dx.as_strided((rows, pad), (n_in + pad, 1), dx.storage_offset() + n_in) == 7).all()
+    return x, w, e, dy, y, dx, dw
+
+
+@pytest.mark.parametrize("out", [BF16, F32])
+@pytest.mark.parametrize("n_in,n_out", [(64, 64), (128, 256), (8, 8), (1, 1), (7, 130), (129, 33), (200, 72),
+                                        (264, 520), (1000, 24), (32, 1000)])
+def test_sizes(ctx, n_in, n_out, out):
+    check_all(ctx, [5, 0, 70, 1, 129, 0], n_in, n_out, out=out, seed=n_in)
+
+
+@pytest.mark.parametrize("counts,unused", [([1], 0), ([0], 1), ([0, 0, 0], 3), ([300], 0), ([16] * 9, 5),
+                                           ([0, 0, 17, 0, 64, 65, 63, 0], 2), ([1] * 200, 0), ([0] * 130 + [40], 7),
+                                           ([2, 3] * 64, 1), ([511, 1, 513], 255), ([], 4), ([0], 0)])
+@pytest.mark.parametrize("n_in,n_out", [(96, 136), (75, 50)])
+def test_groups(ctx, counts, unused, n_in, n_out):
+    check_all(ctx, counts, n_in, n_out, unused, ends=torch.int64, seed=len(counts))
+
+
+@pytest.mark.parametrize("pad,offset", [(8, 0), (8, 8), (3, 0), (0, 1), (2, 2), (4, 4)])
+def test_strides_and_alignment(ctx, pad, offset):
+    check_all(ctx, [40, 9, 0, 100], 160, 72, 3, pad=pad, offset=offset, seed=pad)
+
+
+def test_ends_out_of_order_or_range(ctx):
+    """An end below the one before it makes an empty group; one past the rows is the rows."""
+    for e in ([10, 4, 30, 12], [-3, 5, 1000, 7], [1 << 30, 2, 3, 4], [-1, -2, -3, -4]):
+        check_all(ctx, [10, 0, 20, 5], 72, 40, want_ends=e)
+
+
+@pytest.mark.parametrize("n_in,n_out", [(512, 768), (515, 770)])
+def test_long_contractions(ctx, n_in, n_out):
+    check_all(ctx, [700, 1500, 333], n_in, n_out, out=F32, seed=1)
+
+
+def test_one_gradient_at_a_time(ctx):
+    from paper_2609_34162_amd import ops
+    x, w, e, dy, _, dx, dw = check_all(ctx, [33, 0, 90], 64, 128)
+    a, b = torch.empty_like(dx), torch.empty_like(dw)
+    ops.sdp_grouped_matmul_backward(ctx, None, w, e, dy, a, None)
+    ops.sdp_grouped_matmul_backward(ctx, x, w, e, dy, None, b)
+    assert torch.equal(a, dx) and torch.equal(b, dw)
+
+
+def test_gradient_against_differences(ctx):
+    """y is linear in x and in w: <dx, v> = <y(x + v) - y(x), dy> without a remainder, in 64 bits."""
+    x, w, e, dy, _, dx, dw = check_all(ctx, [33, 0, 90], 64, 128, out=F32)
+    gen = torch.Generator().manual_seed(2)
+    value = lambda x, w: (ops_ref.grouped(x, w, e, F32)[0] * dy.cpu().double()).sum()
+    xd, wd = x.cpu().double(), w.cpu().double()
+    v, u = torch.randn(x.shape, generator=gen).double(), torch.randn(w.shape, generator=gen).double()
+    # dx is rounded to BF16 (2^-9 of each element); dw is in 32 bits over 90 rows
+    got = (dx.cpu().double() * v).sum()
+    assert abs(value(xd + v, wd) - value(xd, wd) - got) <= 2.0 ** -8 * (dx.cpu().double() * v).abs().sum()
+    got = (dw.cpu().double() * u).sum()
+    assert abs(value(xd, wd + u) - value(xd, wd) - got) <= 1e-4 * (dw.cpu().double() * u).abs().sum()
+
+
+def test_same_bits_again(ctx):
+    a = check_all(ctx, [100, 300, 0, 29], 256, 192, seed=4)
+    b = check_all(ctx, [100, 300, 0, 29], 256, 192, seed=4)
+    for x, y in zip(a[4:], b[4:]):
+        assert torch.equal(x, y)
+
+
+def test_infinity_and_nan_stay_in_their_rows_and_groups(ctx):
+    """What one row of x or dy holds reaches its own row of y or dx and its own group of dw only."""
+    from paper_2609_34162_amd import ops
+    gen = torch.Generator().manual_seed(8)
+    for n_in, n_out in ((64, 128), (65, 31)):
+        counts = [20, 45, 17]
+        e = torch.tensor(counts).cumsum(0).cuda()
+        x, dy = strided(gen, 82, n_in, 0), strided(gen, 82, n_out, 0)
+        w = torch.randn((3, n_out, n_in), generator=gen).to(BF16).cuda()
+        x[25], dy[70] = float("nan"), float("inf")
+        y, dx = torch.empty((82, n_out), dtype=BF16, device="cuda"), torch.empty((82, n_in), dtype=BF16, device="cuda")
+        dw = torch.empty((3, n_out, n_in), device="cuda")
+        ops.sdp_grouped_matmul(ctx, x, w, e, y)
+        ops.sdp_grouped_matmul_backward(ctx, x, w, e, dy, dx, dw)
+        rows = torch.arange(82)
+        assert torch.equal(torch.isfinite(y.cpu()).all(1), rows != 25)
+        assert torch.equal(torch.isfinite(dx.cpu()).all(1), rows != 70)
+        assert torch.isfinite(dw[0]).all() and torch.isnan(dw[1]).all() and not torch.isfinite(dw[2]).any()
