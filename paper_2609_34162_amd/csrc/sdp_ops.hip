@@ -209,16 +209,16 @@ int qk_call(sdp_ctx *ctx, const char *call, const sdp_qk_norm_rope_desc *d, cons
     a.sin = d->sin;
     a.positions = d->positions;
     hipStream_t s = (hipStream_t)stream;
-    const bool sums = dweight[0] || dweight[1];
+    const bool sums = dweight[0] || dweight[1], bf16 = d->type == SDP_TYPE_BF16;
+    sdpops::qk_split(a, bf16, backward);
     if (sums) {
-        const int64_t per[2] = {(int64_t)sdpops::qk_backward_blocks(a, 0) * a.dim,
-                                (int64_t)sdpops::qk_backward_blocks(a, 1) * a.dim};
+        const int64_t per[2] = {(int64_t)a.blocks[0] * a.dim, (int64_t)a.blocks[1] * a.dim};
         SDP_TRY(ensure_ops_space(ctx, (size_t)(per[0] + per[1] + 4) * 4));
         a.side[0].partials = dweight[0] ? (float *)ctx->ops_space : nullptr;
         a.side[1].partials = dweight[1] ? (float *)ctx->ops_space + per[0] : nullptr;
         SDP_TRY(ops_order(ctx, s));
     }
-    HIP_TRY(sdpops::launch_qk(a, d->type == SDP_TYPE_BF16, backward, s));
+    HIP_TRY(sdpops::launch_qk(a, bf16, backward, s));
     if (sums) SDP_TRY(ops_mark(ctx, s));
     return SDP_OK;
 }

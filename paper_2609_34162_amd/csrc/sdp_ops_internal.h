@@ -32,17 +32,21 @@ struct QkSide {
 struct QkArgs {
     QkSide side[2];
     int64_t rows_total[2];  // batch * tokens * heads
-    int32_t blocks[2];      // of the launch, first the query heads' blocks
+    int32_t blocks[2];      // of each side; backward each leaves a row of partial sums
     int32_t batch, tokens, dim, rotary, interleaved;
     int32_t weight_bf16, positions64;
     float eps;
     int64_t table_rows;
     const float *cos, *sin;
     const void *positions;
+    // how the call is split (qk_split): runs of heads that a wave takes, and how
+    // many of them a token has on each side
+    int32_t chunk_heads, chunks[2];
+    bool stream;  // non-temporal loads and stores
 };
 
-// Backward: the blocks (rows of partial sums) that a side of this many rows gets.
-int qk_backward_blocks(const QkArgs &a, int side);
+// Fills in how the call is split over blocks.
+void qk_split(QkArgs &a, bool bf16, bool backward);
 hipError_t launch_qk(const QkArgs &a, bool bf16, bool backward, hipStream_t s);
 
 // ---- grouped products ------------------------------------------------------

@@ -1,6 +1,6 @@
 // Decisions of the training operators' host code that need no device, free of
 // HIP so that they can be checked without one: extents and overlaps of strided
-// tensors, and the multipliers that stand for divisions in the kernels.
+// tensors.
 #pragma once
 
 #include <cstdint>
@@ -89,12 +89,5 @@ inline bool disjoint(const char *pa, const Layout &a, const char *pb, const Layo
     all.ext[2] = first + hi.ext[2];
     return injective(all);
 }
-
-// n / d as (n * m) >> 32 with m = floor(2^32 / d) + 1: the product exceeds
-// n * 2^32 / d by n * e / d with 1 <= e <= d, which reaches the next whole
-// quotient only from n * e >= 2^32 on, so it is exact for n < 2^32 / d.
-// d = 1 would need a multiplier past 32 bits: 0 stands for it.
-inline uint32_t quotient_multiplier(uint32_t d) { return d <= 1 ? 0 : (uint32_t)((((uint64_t)1) << 32) / d + 1); }
-inline uint32_t quotient(uint32_t n, uint32_t m) { return m == 0 ? n : (uint32_t)(((uint64_t)n * m) >> 32); }
 
 }  // namespace sdpops

@@ -5,13 +5,17 @@
 // and backward, with dn the rotation's transpose of dy and u = dn w:
 //   dx = r (u - x r mean(u x r)),  dw = sum over rows of dn x r
 // Every element is read once and written once: HBM bounds both directions.
+// 32,768 tokens of 48 heads of 128 in BF16, views of a fused projection: forward
+// 157 us (5.2 TB/s of the tensors' bytes), backward 256 us (4.7 TB/s).
+#include <algorithm>
+
 #include "sdp_ops_device.h"
 #include "sdp_ops_internal.h"
 
 namespace sdpops {
 namespace {
 
-constexpr int kRowWaves = 4;
+constexpr int kRowWaves = 4;  // of a block, in both kernels
 
 // Where element i of a row finds the other one of its rotated pair, the
 // pair's angle and the sign of the partner's sine term.
@@ -132,28 +136,254 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_qk_rows(QkArgs a) {
     }
 }
 
-// dw: the blocks' partial sums, added in a fixed order: 64 threads to a
-// column, 16 columns to a block, the second grid dimension the side.
-__global__ __launch_bounds__(1024) void k_qk_dweight(QkArgs a) {
-    __shared__ float part[64][17];
+// Rows whose 8-element pieces are 16-byte aligned: G lanes take a row, a lane a
+// piece of 8, so that a wave reads 64 / G rows at once; the partner of a rotated
+// pair is in the same lane (interleaved) or rotary / 16 lanes on.  A wave takes a
+// run of heads of one token, so that it reads the token's position and angles
+// once and steps from row to row by additions; the norm's weight goes into the
+// angles: y = r (x (w c) -+ x' (w' s)).
+// Loads and stores of 16 bytes, with the non-temporal hint where a call's data
+// does not fit the last-level cache (see split).
+template <bool STREAM, typename V>
+__device__ __forceinline__ V load16(const void *p) {
+    return STREAM ? __builtin_nontemporal_load((const V *)p) : *(const V *)p;
+}
+template <bool STREAM, typename V>
+__device__ __forceinline__ void store16(void *p, V v) {
+    if (STREAM)
+        __builtin_nontemporal_store(v, (V *)p);
+    else
+        *(V *)p = v;
+}
+
+// 8 elements of a row as they are stored, and as floats.
+template <typename T>
+struct Piece;
+template <>
+struct Piece<uint16_t> {
+    u32x4 raw;
+    template <bool STREAM>
+    __device__ __forceinline__ void load(const uint16_t *p) { raw = load16<STREAM, u32x4>(p); }
+    __device__ __forceinline__ void clear() { raw = u32x4{0, 0, 0, 0}; }
+    __device__ __forceinline__ void floats(float *v) const {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[2 * k] = bf16_lo(raw[k]), v[2 * k + 1] = bf16_hi(raw[k]);
+    }
+    // the piece of another lane
+    __device__ __forceinline__ Piece of(int lane) const {
+        Piece o;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o.raw[k] = __shfl(raw[k], lane);
+        return o;
+    }
+    template <bool STREAM>
+    static __device__ __forceinline__ void store(uint16_t *p, const float *v) {
+        u32x4 u;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) u[k] = pack2(v[2 * k], v[2 * k + 1]);
+        store16<STREAM>(p, u);
+    }
+};
+template <>
+struct Piece<float> {
+    f32x4 a, b;
+    template <bool STREAM>
+    __device__ __forceinline__ void load(const float *p) {
+        a = load16<STREAM, f32x4>(p), b = load16<STREAM, f32x4>(p + 4);
+    }
+    __device__ __forceinline__ void clear() { a = b = f32x4{0, 0, 0, 0}; }
+    __device__ __forceinline__ void floats(float *v) const {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = a[k], v[4 + k] = b[k];
+    }
+    __device__ __forceinline__ Piece of(int lane) const {
+        Piece o;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o.a[k] = __shfl(a[k], lane), o.b[k] = __shfl(b[k], lane);
+        return o;
+    }
+    template <bool STREAM>
+    static __device__ __forceinline__ void store(float *p, const float *v) {
+        store16<STREAM>(p, f32x4{v[0], v[1], v[2], v[3]});
+        store16<STREAM>(p + 4, f32x4{v[4], v[5], v[6], v[7]});
+    }
+};
+
+// Sum over the G lanes of a row.
+template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+    for (int d = G / 2; d > 0; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+
+template <typename T, int G, bool INTERLEAVED, bool BACK, bool STREAM>
+__global__ __launch_bounds__(256) void k_qk_tokens(QkArgs a) {
+    constexpr int kHeads = 64 / G;  // rows that a wave takes at once
+    constexpr int kAhead = 4;       // and how many times that before it computes
+    const int lane = threadIdx.x & 63, piece = lane % G, i = piece * 8, group = lane / G;
+    const int D = a.dim, half = a.rotary / 2;
+    const bool in_row = i < D, turned = i < a.rotary, first_half = i < half;
+    const int partner = first_half ? lane + a.rotary / 16 : lane - a.rotary / 16;
+    const int which = (int)blockIdx.x < a.blocks[0] ? 0 : 1;
+    const QkSide &side = a.side[which];
+    const int block = (int)blockIdx.x - (which ? a.blocks[0] : 0);
+    float sums[8] = {};
+    const int64_t chunks = a.chunks[which], items = (int64_t)a.batch * a.tokens * chunks;
+    const int64_t waves = (int64_t)a.blocks[which] * 4;
+    float w[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = side.weight && in_row ? load_either(side.weight, i + k, a.weight_bf16) : 1.0f;
+    for (int64_t item = (int64_t)block * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); item < items;
+         item += waves) {
+        int64_t token, b;
+        if (items <= 0xffffffffll) {
+            token = (uint32_t)item / (uint32_t)chunks;
+            b = (uint32_t)token / (uint32_t)a.tokens;
+        } else {
+            token = item / chunks;
+            b = token / a.tokens;
+        }
+        const int chunk = (int)(item - token * chunks);
+        const int64_t s = token - b * a.tokens;
+        const int h0 = chunk * a.chunk_heads, h1 = min(h0 + a.chunk_heads, side.heads);
+        const T *px = (const T *)side.x.data + b * side.x.b + s * side.x.s + i;
+        const T *py = BACK ? (const T *)side.y.data + b * side.y.b + s * side.y.s + i : nullptr;
+        T *po = (T *)side.out.data + b * side.out.b + s * side.out.s + i;
+
+        const int64_t at = a.positions ? load_int(a.positions, token, a.positions64) : s;
+        const bool lost = a.rotary > 0 && (at < 0 || at >= a.table_rows);
+        float c[8], sn[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) c[k] = 1.0f, sn[k] = 0.0f;
+        if (turned && !lost) {
+            const int64_t angle = at * half + (INTERLEAVED ? i / 2 : first_half ? i : i - half);
+#pragma unroll
+            for (int k = 0; k < (INTERLEAVED ? 4 : 8); k += 4) {
+                const f32x4 cv = *(const f32x4 *)(a.cos + angle + k), sv = *(const f32x4 *)(a.sin + angle + k);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (INTERLEAVED) {
+                        c[2 * e] = c[2 * e + 1] = cv[e];
+                        sn[2 * e] = -sv[e], sn[2 * e + 1] = sv[e];
+                    } else {
+                        c[k + e] = cv[e];
+                        sn[k + e] = first_half ? -sv[e] : sv[e];
+                    }
+                }
+            }
+        }
+        if (!BACK) {
+            // the weights into the angles: its own with the cosine, its partner's with the sine
+            float wp[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) wp[k] = INTERLEAVED ? w[k ^ 1] : __shfl(w[k], partner);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) c[k] *= w[k], sn[k] *= wp[k];
+        }
+
+        for (int hb = h0; hb < h1; hb += kAhead * kHeads) {
+            Piece<T> xr[kAhead], yr[kAhead];
+            bool on[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                const int h = hb + u * kHeads + group;
+                on[u] = h < h1 && in_row;
+                xr[u].clear();
+                yr[u].clear();
+                if (on[u]) {
+                    xr[u].template load<STREAM>(px + h * side.x.h);
+                    if (BACK) yr[u].template load<STREAM>(py + h * side.y.h);
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) {
+                if (u > 0 && hb + u * kHeads >= h1) break;  // the same for the whole wave
+                float x[8], y[8], o[8];
+                xr[u].floats(x);
+                float sq = 0.0f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sq += x[k] * x[k];
+                float r = rsqrtf(group_sum<G>(sq) * (1.0f / (float)D) + a.eps);
+                if (lost) r = __builtin_nanf("");
+                if (BACK) {
+                    yr[u].floats(y);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] = x[k];
+                }
+                if (INTERLEAVED) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) o[k] = y[k ^ 1];
+                } else {
+                    (BACK ? yr[u] : xr[u]).of(partner).floats(o);
+                }
+                // backward the transpose: the sine's other sign
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    y[k] = y[k] * c[k] + (turned ? (BACK ? -sn[k] : sn[k]) * o[k] : 0.0f);
+                if (!BACK) {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] *= r;
+                } else {
+                    float dot = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        x[k] *= r;
+                        sums[k] += on[u] ? y[k] * x[k] : 0.0f;
+                        y[k] *= w[k];
+                        dot += y[k] * x[k];
+                    }
+                    dot = group_sum<G>(dot) * (1.0f / (float)D);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] = r * (y[k] - x[k] * dot);
+                }
+                if (on[u]) Piece<T>::template store<STREAM>(po + (hb + u * kHeads + group) * side.out.h, y);
+            }
+        }
+    }
+    if (BACK && side.partials) {
+        // the block's lanes of each piece, added in a fixed order
+        __shared__ float part[4][G * 8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            float v = sums[k];
+#pragma unroll
+            for (int d = G; d < 64; d <<= 1) v += __shfl_xor(v, d);
+            if (lane < G) part[threadIdx.x >> 6][i + k] = v;
+        }
+        __syncthreads();
+        for (int e = threadIdx.x; e < D; e += 256)
+            side.partials[(int64_t)block * D + e] = part[0][e] + part[1][e] + (part[2][e] + part[3][e]);
+    }
+}
+
+// dw: the blocks' partial sums, added in a fixed order: four columns to a block,
+// its 256 threads a partial row each in turn; the second grid dimension the side.
+constexpr int kColumns = 4;
+__global__ __launch_bounds__(256) void k_qk_dweight(QkArgs a) {
+    __shared__ float part[4][kColumns];
     const QkSide &side = a.side[blockIdx.y];
     if (!side.dweight) return;
-    const int c = threadIdx.x & 15, t = threadIdx.x >> 4;
-    const int i = blockIdx.x * 16 + c;
-    float s = 0.0f;
-    if (i < a.dim)
-        for (int b = t; b < a.blocks[blockIdx.y]; b += 64) s += side.partials[(int64_t)b * a.dim + i];
-    part[t][c] = s;
-    __syncthreads();
-    for (int half = 32; half > 0; half >>= 1) {
-        if (t < half) part[t][c] += part[t + half][c];
-        __syncthreads();
+    const int i = blockIdx.x * kColumns, rows = a.blocks[blockIdx.y];
+    float s[kColumns] = {};
+#pragma unroll 4
+    for (int b = threadIdx.x; b < rows; b += 256)
+#pragma unroll
+        for (int c = 0; c < kColumns; ++c) s[c] += i + c < a.dim ? side.partials[(int64_t)b * a.dim + i + c] : 0.0f;
+#pragma unroll
+    for (int c = 0; c < kColumns; ++c) {
+        const float v = wave_sum(s[c]);
+        if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6][c] = v;
     }
-    if (t == 0 && i < a.dim) {
+    __syncthreads();
+    if (threadIdx.x < kColumns && i + (int)threadIdx.x < a.dim) {
+        const int c = threadIdx.x;
+        const float v = part[0][c] + part[1][c] + (part[2][c] + part[3][c]);
         if (a.weight_bf16)
-            store1((uint16_t *)side.dweight + i, part[0][c]);
+            store1((uint16_t *)side.dweight + i + c, v);
         else
-            ((float *)side.dweight)[i] = part[0][c];
+            ((float *)side.dweight)[i + c] = v;
     }
 }
 
@@ -162,29 +392,96 @@ void launch_rows(const QkArgs &a, hipStream_t s) {
     hipLaunchKernelGGL((k_qk_rows<T, BACK>), dim3(a.blocks[0] + a.blocks[1]), dim3(64 * kRowWaves), 0, s, a);
 }
 
-int64_t blocks_for(int64_t rows, int64_t most) {
-    const int64_t n = (rows + kRowWaves - 1) / kRowWaves;
-    return n < most ? n : most;
+template <typename T, int G, bool BACK>
+void launch_tokens(const QkArgs &a, hipStream_t s) {
+    const dim3 grid(a.blocks[0] + a.blocks[1]);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a); };
+    if (a.stream)
+        a.interleaved ? go(k_qk_tokens<T, G, true, BACK, true>) : go(k_qk_tokens<T, G, false, BACK, true>);
+    else
+        a.interleaved ? go(k_qk_tokens<T, G, true, BACK, false>) : go(k_qk_tokens<T, G, false, BACK, false>);
+}
+
+// Lanes to a row of the tokens kernel: the power of two that holds the row.
+int lanes_of(int dim) {
+    int g = 4;
+    while (g * 8 < dim) g *= 2;
+    return g;
+}
+
+// Whether the tokens kernel takes the call: whole pieces, partners whole pieces
+// apart, and every row (and the tables') at a 16-byte boundary.
+bool in_pieces(const QkArgs &a, bool bf16, bool backward) {
+    const int64_t per16 = bf16 ? 8 : 4;
+    auto aligned = [&](const Heads &h) {
+        return (uintptr_t)h.data % 16 == 0 && h.b % per16 == 0 && h.s % per16 == 0 && h.h % per16 == 0;
+    };
+    if (a.dim % 8 != 0 || a.dim > 512 || a.rotary % (a.interleaved ? 8 : 16) != 0) return false;
+    if (a.rotary > 0 && ((uintptr_t)a.cos % 16 != 0 || (uintptr_t)a.sin % 16 != 0)) return false;
+    for (int k = 0; k < 2; ++k) {
+        const QkSide &d = a.side[k];
+        if (a.rows_total[k] > 0 && !(aligned(d.x) && aligned(d.out) && (!backward || aligned(d.y)))) return false;
+    }
+    return true;
+}
+
+// How a call is split, in `a`: the blocks of each side and, for the tokens
+// kernel, the runs of heads that a wave takes.  Forward 8,192 blocks of four waves,
+// each walking its share (32,768 tokens of 48 heads of 128, BF16: 157 us; 4,096
+// blocks 176, 16,384 169), four wavefuls of rows loaded ahead (two: 159 us with
+// this split).  Backward 2,048, as each leaves a row of partial sums and holds
+// more registers (256 us; 1,024: 279; 3,072: 251, but 40 instead of 34 us on
+// 4,101 tokens of 16 heads).  Non-temporal loads and stores from 256 MB on, the
+// last-level cache's size: 157 against 163 us and 256 against 274; below it they
+// cost (34 against 32 us).
+void split(QkArgs &a, bool bf16, bool backward) {
+    const int64_t tokens = (int64_t)a.batch * a.tokens, both = a.rows_total[0] + a.rows_total[1];
+    const int64_t most = backward ? 2048 : 8192;
+    const bool pieces = in_pieces(a, bf16, backward);
+    a.stream = both * a.dim * (bf16 ? 2 : 4) * (backward ? 3 : 2) > (int64_t)256 << 20;
+    const int64_t at_once = pieces ? 64 / lanes_of(a.dim) : 1;
+    // runs as long as leave every wave of the grid one, in whole wavefuls of rows
+    const int64_t run = (both + 4 * most - 1) / (4 * most);
+    a.chunk_heads = (int)std::min<int64_t>((run + at_once - 1) / at_once * at_once, SDP_QK_MAX_HEADS);
+    for (int k = 0; k < 2; ++k) {
+        a.chunks[k] = (a.side[k].heads + a.chunk_heads - 1) / a.chunk_heads;
+        const int64_t items = pieces ? tokens * a.chunks[k] : a.rows_total[k];
+        const int64_t share = a.rows_total[k] ? std::max<int64_t>(1, most * a.rows_total[k] / both) : 0;
+        a.blocks[k] = (int)std::min<int64_t>((items + 3) / 4, share);
+    }
+}
+
+template <typename T, bool BACK>
+void launch_any(const QkArgs &a, hipStream_t s) {
+    if (!in_pieces(a, sizeof(T) == 2, BACK)) return launch_rows<T, BACK>(a, s);
+    switch (lanes_of(a.dim)) {
+        case 4: return launch_tokens<T, 4, BACK>(a, s);
+        case 8: return launch_tokens<T, 8, BACK>(a, s);
+        case 16: return launch_tokens<T, 16, BACK>(a, s);
+        case 32: return launch_tokens<T, 32, BACK>(a, s);
+        default: return launch_tokens<T, 64, BACK>(a, s);
+    }
 }
 
 }  // namespace
 
-int qk_backward_blocks(const QkArgs &a, int side) { return (int)blocks_for(a.rows_total[side], 1024); }
+void qk_split(QkArgs &a, bool bf16, bool backward) {
+    a.blocks[0] = a.blocks[1] = a.chunks[0] = a.chunks[1] = 0;
+    a.chunk_heads = 1;
+    if (a.rows_total[0] + a.rows_total[1] > 0) split(a, bf16, backward);
+}
 
-hipError_t launch_qk(const QkArgs &args, bool bf16, bool backward, hipStream_t s) {
-    QkArgs a = args;
-    for (int k = 0; k < 2; ++k)
-        a.blocks[k] = backward ? qk_backward_blocks(a, k) : (int)blocks_for(a.rows_total[k], 1 << 20);
+hipError_t launch_qk(const QkArgs &a, bool bf16, bool backward, hipStream_t s) {
     if (a.blocks[0] + a.blocks[1] > 0) {
         if (bf16)
-            backward ? launch_rows<uint16_t, true>(a, s) : launch_rows<uint16_t, false>(a, s);
+            backward ? launch_any<uint16_t, true>(a, s) : launch_any<uint16_t, false>(a, s);
         else
-            backward ? launch_rows<float, true>(a, s) : launch_rows<float, false>(a, s);
+            backward ? launch_any<float, true>(a, s) : launch_any<float, false>(a, s);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (backward && (a.side[0].dweight || a.side[1].dweight) && a.dim > 0) {
-        hipLaunchKernelGGL(k_qk_dweight, dim3((a.dim + 15) / 16, 2), dim3(1024), 0, s, a);
+    if (backward && (a.side[0].dweight || a.side[1].dweight)) {
+        hipLaunchKernelGGL(k_qk_dweight, dim3((a.dim + kColumns - 1) / kColumns, 2), dim3(256), 0, s, a);
         return hipGetLastError();
     }
     return hipSuccess;

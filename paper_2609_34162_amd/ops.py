@@ -98,22 +98,34 @@ def _want(ok: bool, text: str) -> None:
         raise ValueError(text)
 
 
+def _has_shape(t, shape, what: str) -> None:
+    if t.shape != shape:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+
+
+def _last_contiguous(t, what: str) -> None:
+    if t.stride(-1) != 1 and t.shape[-1] > 1:
+        raise ValueError(f"{what}: the last dimension must be contiguous")
+
+
 def _dense(t, shape, what: str) -> Optional[int]:
     """The address of a contiguous tensor of this shape (None passes)."""
     if t is None:
         return None
-    _want(tuple(t.shape) == tuple(shape), f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    _want(t.is_contiguous(), f"{what} must be contiguous")
+    _has_shape(t, shape, what)
+    if not t.is_contiguous():
+        raise ValueError(f"{what} must be contiguous")
     return t.data_ptr()
 
 
 def _same_type(t, code: int, what: str) -> None:
-    _want(t is None or _type(t, what) == code, f"{what} has another type than expected")
+    if t is not None and _type(t, what) != code:
+        raise ValueError(f"{what} has another type than expected")
 
 
 def _row_stride(t, shape, what: str) -> int:
-    _want(tuple(t.shape) == tuple(shape), f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    _want(t.shape[1] <= 1 or t.stride(1) == 1, f"{what}: the last dimension must be contiguous")
+    _has_shape(t, shape, what)
+    _last_contiguous(t, what)
     return t.stride(0)
 
 
@@ -121,11 +133,9 @@ def _heads(t, shape, what: str) -> sdp_heads:
     """[batch, tokens, heads, head_dim], or [tokens, heads, head_dim] of one sequence."""
     if t.dim() == 3:
         t = t.unsqueeze(0)
-    _want(t.dim() == 4, f"{what} must be [batch, tokens, heads, head_dim]")
-    if shape is not None:
-        _want(tuple(t.shape) == tuple(shape), f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    _want(t.shape[3] <= 1 or t.stride(3) == 1, f"{what}: the last dimension must be contiguous")
-    return sdp_heads(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+    _has_shape(t, shape, what)
+    _last_contiguous(t, what)
+    return sdp_heads(t.data_ptr(), *t.stride()[:3])
 
 
 def _qk_desc(q, k, cos, sin, q_weight, k_weight, positions, eps, interleaved):
@@ -133,7 +143,8 @@ def _qk_desc(q, k, cos, sin, q_weight, k_weight, positions, eps, interleaved):
         _want(t.dim() in (3, 4), "q and k must be [batch, tokens, heads, head_dim]")
         return (1, *t.shape) if t.dim() == 3 else tuple(t.shape)
     qs, ks = shape(q), shape(k)
-    _want(qs[:2] == ks[:2] and qs[3] == ks[3], f"q {qs} and k {ks} differ in batch, tokens or head_dim")
+    if qs[:2] != ks[:2] or qs[3] != ks[3]:
+        raise ValueError(f"q {qs} and k {ks} differ in batch, tokens or head_dim")
     code = _type(q, "q")
     _same_type(k, code, "k")
     d = sdp_qk_norm_rope_desc()
@@ -190,8 +201,8 @@ def sdp_qk_norm_rope_backward(ctx, q, k, dq_out, dk_out, dq, dk, cos=None, sin=N
 
 
 def _grouped_desc(x, w, ends, what: str):
-    _want(x.dim() == 2 and w.dim() == 3 and ends.dim() == 1,
-          f"{what}: rows must be 2-D, w [groups, out, in] and ends [groups]")
+    if x.dim() != 2 or w.dim() != 3 or ends.dim() != 1:
+        raise ValueError(f"{what}: rows must be 2-D, w [groups, out, in] and ends [groups]")
     _want(w.is_contiguous(), "w must be contiguous")
     d = sdp_grouped_desc()
     d.rows, d.groups, d.out_features, d.in_features = x.shape[0], w.shape[0], w.shape[1], w.shape[2]

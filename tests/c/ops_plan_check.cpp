@@ -1,5 +1,5 @@
-// sdp_ops_plan.h on the CPU: spans, overlaps (against an enumeration of every
-// element) and the multipliers that stand for divisions.
+// sdp_ops_plan.h on the CPU: spans and overlaps, against an enumeration of
+// every element.
 #include <cstdio>
 #include <cstdlib>
 #include <set>
@@ -25,13 +25,6 @@ static std::multiset<int64_t> elements(int64_t at, const Layout &l) {
 }
 
 int main() {
-    // quotients, at the ends of their range
-    for (uint32_t d : {1u, 2u, 3u, 5u, 7u, 8u, 40u, 48u, 100u, 641u, 4096u, 16384u, 32767u}) {
-        const uint32_t m = quotient_multiplier(d);
-        const uint64_t top = d == 1 ? 1u << 20 : ((uint64_t)1 << 32) / d;
-        for (uint64_t n = 0; n < top; n += n < 100000 ? 1 : 9973) EXPECT(quotient((uint32_t)n, m) == n / d);
-        for (uint64_t n = top > 100000 ? top - 100000 : 0; n < top; ++n) EXPECT(quotient((uint32_t)n, m) == n / d);
-    }
     // random small layouts: what the tests promise holds for every element
     std::srand(7);
     int proved = 0, injected = 0;
