@@ -39,9 +39,9 @@ struct QkArgs {
     int64_t table_rows;
     const float *cos, *sin;
     const void *positions;
-    // how the call is split (qk_split): runs of heads that a wave takes, and how
-    // many of them a token has on each side
-    int32_t chunk_heads, chunks[2];
+    // how the call is split (qk_split): runs of heads that a wave takes, how many
+    // of them a token has on each side, and the heads that it reads at once (log 2)
+    int32_t chunk_heads, chunks[2], heads_log[2];
     bool stream;  // non-temporal loads and stores
 };
 

@@ -137,11 +137,13 @@ __global__ __launch_bounds__(64 * kRowWaves) void k_qk_rows(QkArgs a) {
 }
 
 // Rows whose 8-element pieces are 16-byte aligned: G lanes take a row, a lane a
-// piece of 8, so that a wave reads 64 / G rows at once; the partner of a rotated
-// pair is in the same lane (interleaved) or rotary / 16 lanes on.  A wave takes a
-// run of heads of one token, so that it reads the token's position and angles
-// once and steps from row to row by additions; the norm's weight goes into the
-// angles: y = r (x (w c) -+ x' (w' s)).
+// piece of 8, so that a wave reads 64 / G rows at once; the partners of a lane's
+// elements are in the same lane (interleaved), or each half piece's rotary / 8
+// half pieces on.  A wave takes a
+// run of heads of one token (of several where a token has fewer heads than rows
+// fit), so that it reads a token's position and angles once and steps from row to
+// row by additions; the norm's weight goes into the angles:
+// y = r (x (w c) -+ x' (w' s)).
 // Loads and stores of 16 bytes, with the non-temporal hint where a call's data
 // does not fit the last-level cache (see split).
 template <bool STREAM, typename V>
@@ -169,11 +171,12 @@ struct Piece<uint16_t> {
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[2 * k] = bf16_lo(raw[k]), v[2 * k + 1] = bf16_hi(raw[k]);
     }
-    // the piece of another lane
-    __device__ __forceinline__ Piece of(int lane) const {
+    // each half from another lane, SWAP: the other half there
+    template <bool SWAP>
+    __device__ __forceinline__ Piece partners(const int *lane) const {
         Piece o;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o.raw[k] = __shfl(raw[k], lane);
+        for (int k = 0; k < 4; ++k) o.raw[k] = __shfl(raw[SWAP ? k ^ 2 : k], lane[SWAP ? k / 2 : 0]);
         return o;
     }
     template <bool STREAM>
@@ -196,10 +199,14 @@ struct Piece<float> {
 #pragma unroll
         for (int k = 0; k < 4; ++k) v[k] = a[k], v[4 + k] = b[k];
     }
-    __device__ __forceinline__ Piece of(int lane) const {
+    template <bool SWAP>
+    __device__ __forceinline__ Piece partners(const int *lane) const {
         Piece o;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) o.a[k] = __shfl(a[k], lane), o.b[k] = __shfl(b[k], lane);
+        for (int k = 0; k < 4; ++k) {
+            o.a[k] = __shfl(SWAP ? b[k] : a[k], lane[0]);
+            o.b[k] = __shfl(SWAP ? a[k] : b[k], lane[SWAP ? 1 : 0]);
+        }
         return o;
     }
     template <bool STREAM>
@@ -217,50 +224,77 @@ __device__ __forceinline__ float group_sum(float v) {
     return v;
 }
 
-template <typename T, int G, bool INTERLEAVED, bool BACK, bool STREAM>
+// How a rotated pair lies in a row: neighbours; or half the rotated dimensions
+// apart, an even or an odd number of half pieces.
+enum Pairs { kNeighbours, kHalves, kHalvesOdd };
+
+template <typename T, int G, Pairs PAIRS, bool BACK, bool STREAM>
 __global__ __launch_bounds__(256) void k_qk_tokens(QkArgs a) {
-    constexpr int kHeads = 64 / G;  // rows that a wave takes at once
-    constexpr int kAhead = 4;       // and how many times that before it computes
-    const int lane = threadIdx.x & 63, piece = lane % G, i = piece * 8, group = lane / G;
+    constexpr bool INTERLEAVED = PAIRS == kNeighbours, kSwap = PAIRS == kHalvesOdd;
+    constexpr int kAhead = 4;  // how many wavefuls of rows are loaded before they are worked on
+    const int lane = threadIdx.x & 63, piece = lane % G, i = piece * 8;
     const int D = a.dim, half = a.rotary / 2;
-    const bool in_row = i < D, turned = i < a.rotary, first_half = i < half;
-    const int partner = first_half ? lane + a.rotary / 16 : lane - a.rotary / 16;
+    const bool in_row = i < D, turned = i < a.rotary;
+    // of each half piece (of both where they cannot differ): whether it comes first
+    // in its pairs, and the lane that has its partner
+    constexpr int kOwn = kSwap ? 1 : 0;
+    const bool first[2] = {i < half, i + 4 < half};
+    int partner[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+        partner[j] = lane - piece + (first[j] ? 2 * piece + j + half / 4 : 2 * piece + j - half / 4) / 2;
     const int which = (int)blockIdx.x < a.blocks[0] ? 0 : 1;
     const QkSide &side = a.side[which];
     const int block = (int)blockIdx.x - (which ? a.blocks[0] : 0);
     float sums[8] = {};
-    const int64_t chunks = a.chunks[which], items = (int64_t)a.batch * a.tokens * chunks;
+    // the wave's 64 / G rows: `at_once` heads (a power of two) of each of several tokens
+    const int at_once = 1 << a.heads_log[which], tokens_log = __builtin_ctz(64 / G) - a.heads_log[which];
+    const int head = lane / G & (at_once - 1), token_in_wave = lane / G >> a.heads_log[which];
+    const int64_t all_tokens = (int64_t)a.batch * a.tokens;
+    const int64_t chunks = a.chunks[which];
     const int64_t waves = (int64_t)a.blocks[which] * 4;
     float w[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) w[k] = side.weight && in_row ? load_either(side.weight, i + k, a.weight_bf16) : 1.0f;
-    for (int64_t item = (int64_t)block * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); item < items;
-         item += waves) {
-        int64_t token, b;
-        if (items <= 0xffffffffll) {
-            token = (uint32_t)item / (uint32_t)chunks;
-            b = (uint32_t)token / (uint32_t)a.tokens;
-        } else {
-            token = item / chunks;
-            b = token / a.tokens;
+    // the wave's item: a run of heads of the tokens from (b0, s0) on; from one
+    // item to the next by additions, as divisions would cost more than a row
+    int64_t item = (int64_t)block * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    int64_t group0 = item / chunks, left = all_tokens - (group0 << tokens_log);  // tokens from the first one on
+    int chunk = (int)(item - group0 * chunks);
+    int64_t b0 = (group0 << tokens_log) / a.tokens, s0 = (group0 << tokens_log) - b0 * a.tokens;
+    const int64_t more_groups = waves / chunks, more_b = (more_groups << tokens_log) / a.tokens,
+                  more_s = (more_groups << tokens_log) - more_b * a.tokens;
+    const int more_chunks = (int)(waves - more_groups * chunks);
+    for (; left > 0;
+         chunk += more_chunks, left -= more_groups << tokens_log, b0 += more_b, s0 += more_s) {
+        if (chunk >= chunks) {
+            chunk -= (int)chunks;
+            left -= 1 << tokens_log;
+            s0 += 1 << tokens_log;
         }
-        const int chunk = (int)(item - token * chunks);
-        const int64_t s = token - b * a.tokens;
+        for (; s0 >= a.tokens; ++b0) s0 -= a.tokens;
+        if (left <= 0) break;
+        const bool has_token = token_in_wave < left;
+        int64_t b = b0, s = s0;
+        if (tokens_log > 0) {
+            s += has_token ? token_in_wave : 0;
+            for (; s >= a.tokens; ++b) s -= a.tokens;
+        }
+        const int64_t at = a.positions ? load_int(a.positions, b * a.tokens + s, a.positions64) : s;
         const int h0 = chunk * a.chunk_heads, h1 = min(h0 + a.chunk_heads, side.heads);
         const T *px = (const T *)side.x.data + b * side.x.b + s * side.x.s + i;
         const T *py = BACK ? (const T *)side.y.data + b * side.y.b + s * side.y.s + i : nullptr;
         T *po = (T *)side.out.data + b * side.out.b + s * side.out.s + i;
 
-        const int64_t at = a.positions ? load_int(a.positions, token, a.positions64) : s;
         const bool lost = a.rotary > 0 && (at < 0 || at >= a.table_rows);
         float c[8], sn[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) c[k] = 1.0f, sn[k] = 0.0f;
         if (turned && !lost) {
-            const int64_t angle = at * half + (INTERLEAVED ? i / 2 : first_half ? i : i - half);
 #pragma unroll
             for (int k = 0; k < (INTERLEAVED ? 4 : 8); k += 4) {
-                const f32x4 cv = *(const f32x4 *)(a.cos + angle + k), sv = *(const f32x4 *)(a.sin + angle + k);
+                const int64_t angle = at * half + (INTERLEAVED ? i / 2 : first[k / 4 * kOwn] ? i + k : i + k - half);
+                const f32x4 cv = *(const f32x4 *)(a.cos + angle), sv = *(const f32x4 *)(a.sin + angle);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     if (INTERLEAVED) {
@@ -268,7 +302,7 @@ __global__ __launch_bounds__(256) void k_qk_tokens(QkArgs a) {
                         sn[2 * e] = -sv[e], sn[2 * e + 1] = sv[e];
                     } else {
                         c[k + e] = cv[e];
-                        sn[k + e] = first_half ? -sv[e] : sv[e];
+                        sn[k + e] = first[k / 4 * kOwn] ? -sv[e] : sv[e];
                     }
                 }
             }
@@ -277,18 +311,18 @@ __global__ __launch_bounds__(256) void k_qk_tokens(QkArgs a) {
             // the weights into the angles: its own with the cosine, its partner's with the sine
             float wp[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) wp[k] = INTERLEAVED ? w[k ^ 1] : __shfl(w[k], partner);
+            for (int k = 0; k < 8; ++k) wp[k] = INTERLEAVED ? w[k ^ 1] : __shfl(w[kSwap ? k ^ 4 : k], partner[k / 4 * kOwn]);
 #pragma unroll
             for (int k = 0; k < 8; ++k) c[k] *= w[k], sn[k] *= wp[k];
         }
 
-        for (int hb = h0; hb < h1; hb += kAhead * kHeads) {
+        for (int hb = h0; hb < h1; hb += kAhead * at_once) {
             Piece<T> xr[kAhead], yr[kAhead];
             bool on[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const int h = hb + u * kHeads + group;
-                on[u] = h < h1 && in_row;
+                const int h = hb + u * at_once + head;
+                on[u] = h < h1 && in_row && has_token;
                 xr[u].clear();
                 yr[u].clear();
                 if (on[u]) {
@@ -298,7 +332,7 @@ __global__ __launch_bounds__(256) void k_qk_tokens(QkArgs a) {
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                if (u > 0 && hb + u * kHeads >= h1) break;  // the same for the whole wave
+                if (u > 0 && hb + u * at_once >= h1) break;  // the same for the whole wave
                 float x[8], y[8], o[8];
                 xr[u].floats(x);
                 float sq = 0.0f;
@@ -316,7 +350,7 @@ __global__ __launch_bounds__(256) void k_qk_tokens(QkArgs a) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) o[k] = y[k ^ 1];
                 } else {
-                    (BACK ? yr[u] : xr[u]).of(partner).floats(o);
+                    (BACK ? yr[u] : xr[u]).template partners<kSwap>(partner).floats(o);
                 }
                 // backward the transpose: the sine's other sign
 #pragma unroll
@@ -338,7 +372,7 @@ __global__ __launch_bounds__(256) void k_qk_tokens(QkArgs a) {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) y[k] = r * (y[k] - x[k] * dot);
                 }
-                if (on[u]) Piece<T>::template store<STREAM>(po + (hb + u * kHeads + group) * side.out.h, y);
+                if (on[u]) Piece<T>::template store<STREAM>(po + (hb + u * at_once + head) * side.out.h, y);
             }
         }
     }
@@ -396,10 +430,15 @@ template <typename T, int G, bool BACK>
 void launch_tokens(const QkArgs &a, hipStream_t s) {
     const dim3 grid(a.blocks[0] + a.blocks[1]);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a); };
+    const bool odd = a.rotary / 8 % 2 != 0;
     if (a.stream)
-        a.interleaved ? go(k_qk_tokens<T, G, true, BACK, true>) : go(k_qk_tokens<T, G, false, BACK, true>);
+        a.interleaved ? go(k_qk_tokens<T, G, kNeighbours, BACK, true>)
+        : odd         ? go(k_qk_tokens<T, G, kHalvesOdd, BACK, true>)
+                      : go(k_qk_tokens<T, G, kHalves, BACK, true>);
     else
-        a.interleaved ? go(k_qk_tokens<T, G, true, BACK, false>) : go(k_qk_tokens<T, G, false, BACK, false>);
+        a.interleaved ? go(k_qk_tokens<T, G, kNeighbours, BACK, false>)
+        : odd         ? go(k_qk_tokens<T, G, kHalvesOdd, BACK, false>)
+                      : go(k_qk_tokens<T, G, kHalves, BACK, false>);
 }
 
 // Lanes to a row of the tokens kernel: the power of two that holds the row.
@@ -409,14 +448,14 @@ int lanes_of(int dim) {
     return g;
 }
 
-// Whether the tokens kernel takes the call: whole pieces, partners whole pieces
-// apart, and every row (and the tables') at a 16-byte boundary.
+// Whether the tokens kernel takes the call: whole pieces, partners whole half
+// pieces apart, and every row (and the tables') at a 16-byte boundary.
 bool in_pieces(const QkArgs &a, bool bf16, bool backward) {
     const int64_t per16 = bf16 ? 8 : 4;
     auto aligned = [&](const Heads &h) {
         return (uintptr_t)h.data % 16 == 0 && h.b % per16 == 0 && h.s % per16 == 0 && h.h % per16 == 0;
     };
-    if (a.dim % 8 != 0 || a.dim > 512 || a.rotary % (a.interleaved ? 8 : 16) != 0) return false;
+    if (a.dim % 8 != 0 || a.dim > 512 || a.rotary % 8 != 0) return false;
     if (a.rotary > 0 && ((uintptr_t)a.cos % 16 != 0 || (uintptr_t)a.sin % 16 != 0)) return false;
     for (int k = 0; k < 2; ++k) {
         const QkSide &d = a.side[k];
@@ -439,13 +478,16 @@ void split(QkArgs &a, bool bf16, bool backward) {
     const int64_t most = backward ? 2048 : 8192;
     const bool pieces = in_pieces(a, bf16, backward);
     a.stream = both * a.dim * (bf16 ? 2 : 4) * (backward ? 3 : 2) > (int64_t)256 << 20;
-    const int64_t at_once = pieces ? 64 / lanes_of(a.dim) : 1;
     // runs as long as leave every wave of the grid one, in whole wavefuls of rows
+    const int fit = pieces ? 64 / lanes_of(a.dim) : 1;
     const int64_t run = (both + 4 * most - 1) / (4 * most);
-    a.chunk_heads = (int)std::min<int64_t>((run + at_once - 1) / at_once * at_once, SDP_QK_MAX_HEADS);
+    a.chunk_heads = (int)std::min<int64_t>((run + fit - 1) / fit * fit, SDP_QK_MAX_HEADS);
     for (int k = 0; k < 2; ++k) {
+        a.heads_log[k] = 0;
+        while ((1 << a.heads_log[k]) < std::min(fit, a.side[k].heads)) ++a.heads_log[k];
+        const int tokens_at_once = fit >> a.heads_log[k];
         a.chunks[k] = (a.side[k].heads + a.chunk_heads - 1) / a.chunk_heads;
-        const int64_t items = pieces ? tokens * a.chunks[k] : a.rows_total[k];
+        const int64_t items = pieces ? (tokens + tokens_at_once - 1) / tokens_at_once * a.chunks[k] : a.rows_total[k];
         const int64_t share = a.rows_total[k] ? std::max<int64_t>(1, most * a.rows_total[k] / both) : 0;
         a.blocks[k] = (int)std::min<int64_t>((items + 3) / 4, share);
     }
