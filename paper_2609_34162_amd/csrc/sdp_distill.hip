@@ -1,10 +1,21 @@
 // gfx950 kernels of sdp_distill_loss and its backward.
 //
-// A row needs max z and the two sums S_tau = sum exp((z - max) / tau) and
-// S_1 = sum exp(z - max) (one where tau = 1), then its loss from a few
+// A row needs its largest logit and the two sums S_tau = sum exp((z - max) / tau)
+// and S_1 = sum exp(z - max) (one where tau = 1), then its loss from a few
 // gathered logits, and its gradient
 //   g (a tau (exp(z / tau - L_tau) - q) + b (exp(z - L_1) - [label]))
-// HBM bounds it: each logit is read once and each gradient written once.
+// The floor is the memory's: each logit read once and each gradient written
+// once.  Two ways there:
+//  - resident: a block holds a whole row in its registers (a compute unit's hold
+//    512 KB, a row of 151,936 BF16 logits 304 KB), so the gradient needs no
+//    second read.  While it writes a row's gradient it loads the next row.
+//  - split: blocks share a row; one pass leaves each part's sums, a second one
+//    joins them and writes the loss and, where it is wanted, the gradient.
+// An exponential takes as long as four multiplications, and two for each logit and
+// pass would bound the resident kernel.  Where tau is 2, 3 or 4 (kernels' POWER),
+// exp(z) is that power of exp(z / tau) instead.
+#include <algorithm>
+
 #include "sdp_ops_device.h"
 #include "sdp_ops_internal.h"
 
@@ -12,176 +23,677 @@ namespace sdpops {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896341f;
+constexpr float kLn2 = 0.693147180559945309f;
 constexpr float kNegInf = -__builtin_huge_valf();
 
-__device__ __forceinline__ float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// max of z and the sums of exp((z - max) / tau) and exp(z - max) over what
-// was seen; max = -inf (nothing but -inf) goes with sums of 0.
-struct Stats {
-    float top, s_tau, s_one;
+// ---- 16 bytes of a row ---------------------------------------------------------
+
+// A row starts wherever its stride puts it, so 16-byte accesses are only aligned
+// to an element.
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+
+template <typename T>
+constexpr int kPer = 16 / (int)sizeof(T);
+
+template <typename T>
+__device__ __forceinline__ u32x4 load_piece(const T *p) {
+    return *(const u32x4_any *)p;
+}
+template <typename T>
+__device__ __forceinline__ u32x4 load_piece_once(const T *p) {
+    return __builtin_nontemporal_load((const u32x4_any *)p);
+}
+__device__ __forceinline__ void floats_of(u32x4 r, const uint16_t *, float *v) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[2 * k] = bf16_lo(r[k]), v[2 * k + 1] = bf16_hi(r[k]);
+}
+__device__ __forceinline__ void floats_of(u32x4 r, const float *, float *v) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = __uint_as_float(r[k]);
+}
+__device__ __forceinline__ void store_piece(uint16_t *p, const float *v) {
+    u32x4 u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) u[k] = pack2(v[2 * k], v[2 * k + 1]);
+    __builtin_nontemporal_store(u, (u32x4_any *)p);
+}
+__device__ __forceinline__ void store_piece(float *p, const float *v) {
+    u32x4 u;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) u[k] = __float_as_uint(v[k]);
+    __builtin_nontemporal_store(u, (u32x4_any *)p);
+}
+// The compiler is not to keep a piece's floats from one use of it to the next:
+// a held row has registers for its pieces only.
+__device__ __forceinline__ void forget(u32x4 &r) { asm volatile("" : "+v"(r)); }
+
+// Eight or four times minus infinity.
+template <typename T>
+__device__ __forceinline__ u32x4 nothing() {
+    const uint32_t u = sizeof(T) == 2 ? 0xff80ff80u : 0xff800000u;
+    return u32x4{u, u, u, u};
+}
+
+// ---- sums ------------------------------------------------------------------------
+
+// What a kernel does with the two exponents z / tau and z.  POWER 0: only one of
+// them is needed; 1: both, two exponentials; 2, 3, 4: both, tau being that number.
+template <int POWER>
+__device__ __forceinline__ float power(float e) {
+    if (POWER == 2) return e * e;
+    if (POWER == 3) return e * e * e;
+    return (e * e) * (e * e);
+}
+
+// The largest of some logits and the sums of 2^((z - top) c) for c = log2(e) / tau
+// and log2(e); top = -inf (nothing but -inf) goes with sums of 0 against 0.
+// Differences come first: logits as low as the type goes overflow in a product.
+struct Sums {
+    float top, tau, one;
 };
 
-__device__ __forceinline__ Stats nothing() { return {kNegInf, 0.0f, 0.0f}; }
+__device__ __forceinline__ float against(float top) { return top == kNegInf ? 0.0f : top; }
 
-// Sums of a shifted to another maximum; a part that saw nothing adds nothing.
-__device__ __forceinline__ Stats join(Stats a, Stats b, float inv_tau) {
-    const float top = fmaxf(a.top, b.top);
-    const float ref = top == kNegInf ? 0.0f : top;
+__device__ __forceinline__ Sums join(Sums a, Sums b, float c_tau) {
+    const float top = fmaxf(a.top, b.top), ref = against(top);
     const float da = a.top - ref, db = b.top - ref;
-    return {top, a.s_tau * exp_of(da * inv_tau) + b.s_tau * exp_of(db * inv_tau),
-            a.s_one * exp_of(da) + b.s_one * exp_of(db)};
+    return {top, a.tau * exp2_of(da * c_tau) + b.tau * exp2_of(db * c_tau),
+            a.one * exp2_of(da * kLog2e) + b.one * exp2_of(db * kLog2e)};
 }
 
-__device__ __forceinline__ void add(Stats &st, float z, float inv_tau) {
-    if (!(z <= st.top)) st = join(st, {z, 0.0f, 0.0f}, inv_tau);
-    const float d = z - (st.top == kNegInf ? 0.0f : st.top);
-    st.s_tau += exp_of(d * inv_tau);
-    st.s_one += exp_of(d);
+__device__ __forceinline__ Sums wave_join(Sums s, float c_tau) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1)
+        s = join(s, {__shfl_xor(s.top, d), __shfl_xor(s.tau, d), __shfl_xor(s.one, d)}, c_tau);
+    return s;
 }
 
-// The teacher's side of a row, in LDS: entries that are there, and their q.
-template <int kMax>
-struct Teacher {
-    int32_t index[kMax];
-    float q[kMax];     // t / tau, then q
-    float log_q[kMax];
-    float z[kMax];
+// L = log of a sum against top, and 1 / sum.
+__device__ __forceinline__ float log_of(float sum, float top, float scale) { return logf(sum) + against(top) * scale; }
+
+// ---- the teacher and the label of a row --------------------------------------------
+
+struct Row {
+    float log_sum;     // of the teacher's exp(t / tau)
+    bool has_teacher, has_label, bad;
+    int32_t label;     // -1: none
 };
 
-constexpr int kThreads = 256;
-
-template <bool SUM>
-__device__ float block_reduce(float v, float *scratch) {
-    v = SUM ? wave_sum(v) : wave_max(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float r = scratch[0];
-    for (int w = 1; w < (int)blockDim.x / 64; ++w) r = SUM ? r + scratch[w] : fmaxf(r, scratch[w]);
+// Found by one whole wave.
+__device__ Row row_of(const DistillArgs &a, int64_t row) {
+    const int lane = threadIdx.x & 63, K = a.k;
+    float top = kNegInf, bad = 0.0f;
+    for (int j = lane; j < K; j += 64) {
+        const int64_t idx = load_int(a.teacher_index, row * K + j, a.index64);
+        if (idx >= a.vocab) bad = 1.0f;
+        if (idx >= 0) top = fmaxf(top, load_either(a.teacher_logits, row * K + j, a.teacher_bf16) * a.inv_tau);
+    }
+    top = wave_max(top);
+    float sum = 0.0f;
+    for (int j = lane; j < K; j += 64)
+        if (load_int(a.teacher_index, row * K + j, a.index64) >= 0)
+            sum += exp2_of((load_either(a.teacher_logits, row * K + j, a.teacher_bf16) * a.inv_tau - against(top)) *
+                           kLog2e);
+    sum = wave_sum(sum);
+    Row r;
+    r.log_sum = logf(sum) + against(top);
+    // a NaN among the teacher's logits leaves top alone and makes the sum NaN
+    r.has_teacher = a.distill_weight != 0.0f && (top != kNegInf || sum != 0.0f);
+    int64_t label = a.labels && a.label_weight != 0.0f ? load_int(a.labels, row, a.index64) : -1;
+    if (label >= a.vocab) bad = 1.0f, label = -1;
+    r.label = (int32_t)label;
+    r.has_label = label >= 0;
+    if (label < 0) r.label = -1;
+    r.bad = wave_max(bad) != 0.0f;
     return r;
 }
 
-// One block walks one row: statistics, loss, gradient.
-template <typename T, bool BACK>
-__global__ __launch_bounds__(kThreads) void k_distill_rows(DistillArgs a) {
-    __shared__ Teacher<SDP_DISTILL_MAX_K> t;
-    __shared__ float scratch[kThreads / 64];
-    __shared__ Stats waves[kThreads / 64];
+// Entry j: its place in the row (-1: not there, or past the vocabulary), q and log q.
+__device__ __forceinline__ int32_t entry(const DistillArgs &a, int64_t row, const Row &r, int j, float *q,
+                                         float *log_q) {
+    const int64_t idx = load_int(a.teacher_index, row * a.k + j, a.index64);
+    *log_q = load_either(a.teacher_logits, row * a.k + j, a.teacher_bf16) * a.inv_tau - r.log_sum;
+    *q = idx >= 0 ? exp2_of(*log_q * kLog2e) : 0.0f;
+    return idx >= 0 && idx < a.vocab ? (int32_t)idx : -1;
+}
+
+// What one part of a row says to its loss: sum of q (log q - z / tau) and of q
+// over the entries in [v0, v1), and the label's logit.
+struct Terms {
+    float dot, q, z_label;
+};
+
+__device__ Terms wave_terms(const DistillArgs &a, int64_t row, const Row &r, float (*z_at)(const void *, int64_t),
+                            const void *z, int64_t v0, int64_t v1) {
+    const int lane = threadIdx.x & 63;
+    Terms t{0.0f, 0.0f, 0.0f};
+    if (r.has_teacher)
+        for (int j = lane; j < a.k; j += 64) {
+            float q, log_q;
+            const int32_t v = entry(a, row, r, j, &q, &log_q);
+            if (v < v0 || v >= v1 || q == 0.0f) continue;
+            t.dot += q * (log_q - z_at(z, v) * a.inv_tau);
+            t.q += q;
+        }
+    t.dot = wave_sum(t.dot);
+    t.q = wave_sum(t.q);
+    if (r.label >= v0 && r.label < v1) t.z_label = z_at(z, r.label);
+    return t;
+}
+
+template <typename T>
+__device__ float z_at(const void *z, int64_t v) {
+    return load1((const T *)z + v);
+}
+
+__device__ float loss_of(const DistillArgs &a, const Row &r, const Terms &t, float l_tau, float l_one) {
+    float loss = 0.0f;
+    if (r.has_teacher) loss = a.distill_weight * a.tau * a.tau * (t.dot + t.q * l_tau);
+    if (r.has_label) loss += a.label_weight * (l_one - t.z_label);
+    return r.bad ? __builtin_nanf("") : loss;
+}
+
+// ---- the gradient --------------------------------------------------------------------
+
+// d = k_tau 2^((z s - r_tau) c) + k_one 2^((z - r_one) log2(e)), before the terms of
+// the entries and the label; POWER 0: the first alone, 2 to 4: the second is that
+// power of the first.  From the sums of the row r = top, s = 1 and c = log2(e) / tau;
+// from their logarithms (BACK) r_tau = L_tau, r_one = L_1, s = 1 / tau and c = log2(e).
+struct Slope {
+    float s, r_tau, c, k_tau, r_one, k_one;
+    float g_tau, g_one;  // what the entries' q and the label's 1 are multiplied by
+};
+
+template <int POWER, bool BACK>
+__device__ Slope slope_of(const DistillArgs &a, const Row &r, float g, Sums sums, float l_tau, float l_one) {
+    Slope d;
+    g = r.bad ? __builtin_nanf("") : g;
+    d.g_tau = r.has_teacher || r.bad ? g * a.distill_weight * a.tau : 0.0f;
+    d.g_one = r.has_label || r.bad ? g * a.label_weight : 0.0f;
+    const float ref = against(sums.top);
+    d.s = BACK ? a.inv_tau : 1.0f;
+    d.c = BACK ? kLog2e : a.inv_tau * kLog2e;
+    d.r_tau = BACK ? l_tau : ref;
+    d.r_one = BACK ? l_one : ref;
+    d.k_tau = d.g_tau == 0.0f ? 0.0f : BACK ? d.g_tau : d.g_tau / sums.tau;
+    d.k_one = d.g_one == 0.0f ? 0.0f : BACK ? d.g_one : d.g_one / sums.one;
+    if (POWER == 0) {
+        // one of the terms is off, or both have the same exponent
+        if (d.g_tau == 0.0f && d.g_one != 0.0f) d.s = 1.0f, d.c = kLog2e, d.r_tau = d.r_one;
+        d.k_tau += d.k_one;
+    }
+    // exp(z - L_1) = exp(z / tau - L_tau)^tau exp(tau L_tau - L_1)
+    if (BACK && POWER >= 2 && d.k_one != 0.0f)
+        d.k_one *= exp2_of(__builtin_fmaf((float)POWER, l_tau, -l_one) * kLog2e);
+    return d;
+}
+
+template <int POWER, bool BACK>
+__device__ __forceinline__ float slope_at(const Slope &d, float z) {
+    const float diff = BACK ? __builtin_fmaf(z, d.s, -d.r_tau) : z - d.r_tau;
+    const float e = exp2_of(diff * d.c);
+    if (POWER == 0) return d.k_tau * e;
+    if (POWER == 1) return d.k_tau * e + d.k_one * exp2_of((BACK ? z - d.r_one : diff) * kLog2e);
+    return d.k_tau * e + d.k_one * power<POWER>(e);
+}
+
+// The entries of a row that a block's gradient has to correct, in LDS.
+struct Entries {
+    int32_t index[SDP_DISTILL_MAX_K + 1];  // -1: not in the block's part; [k]: the label
+    float q[SDP_DISTILL_MAX_K + 1];
+    float z[SDP_DISTILL_MAX_K + 1];
+};
+
+// By one whole wave, before the block writes anything: dlogits may be logits.
+template <typename T>
+__device__ void gather_entries(const DistillArgs &a, int64_t row, const Row &r, const T *z, int64_t v0, int64_t v1,
+                               Entries &e) {
+    for (int j = threadIdx.x & 63; j <= a.k; j += 64) {
+        float q = 0.0f, log_q;
+        int32_t v = r.label;
+        if (j < a.k) v = r.has_teacher ? entry(a, row, r, j, &q, &log_q) : -1;
+        if (v < v0 || v >= v1) v = -1;
+        e.index[j] = v;
+        e.q[j] = q;
+        e.z[j] = v >= 0 ? load1(z + v) : 0.0f;
+    }
+}
+
+// After the block has written its part (and met): the entries' elements anew,
+// each with all that names it, so that elements named twice are written alike.
+template <typename T, int POWER, bool BACK>
+__device__ void correct_entries(const DistillArgs &a, const Row &r, const Slope &d, const Entries &e, T *dz) {
+    for (int j = threadIdx.x; j <= a.k; j += blockDim.x) {
+        const int32_t v = e.index[j];
+        if (v < 0) continue;
+        float q = 0.0f;
+        for (int i = 0; i < a.k; ++i) q += e.index[i] == v ? e.q[i] : 0.0f;
+        float s = slope_at<POWER, BACK>(d, e.z[j]) - d.g_tau * q;
+        if (v == r.label) s -= d.g_one;
+        store1(dz + v, s);
+    }
+}
+
+// ---- split rows ------------------------------------------------------------------------
+
+constexpr int kSplitThreads = 256, kSplitAhead = 4;
+
+struct Part {
+    int64_t p0, p1;  // 16-byte pieces
+    int64_t v0, v1;  // elements (the last part has the row's last few)
+};
+template <typename T>
+__device__ __forceinline__ Part part_of(const DistillArgs &a, int part, int parts) {
+    const int64_t pieces = a.vocab / kPer<T>, each = (pieces + parts - 1) / parts;
+    Part p;
+    p.p0 = part * each < pieces ? part * each : pieces;
+    p.p1 = p.p0 + each < pieces ? p.p0 + each : pieces;
+    p.v0 = p.p0 * kPer<T>;
+    p.v1 = part == parts - 1 ? a.vocab : p.p1 * kPer<T>;
+    return p;
+}
+
+// Adds kN logits, the largest of them and of s.top being `top`, to sums against it.
+template <int kN, int POWER>
+__device__ __forceinline__ void add_against(Sums &s, const float *z, float ref, float c_tau) {
+#pragma unroll
+    for (int k = 0; k < kN; ++k) {
+        const float d = z[k] - ref, e = exp2_of(d * c_tau);
+        s.tau += e;
+        if (POWER == 1) s.one += exp2_of(d * kLog2e);
+        if (POWER >= 2) s.one += power<POWER>(e);
+    }
+}
+
+// Adds kN logits to a thread's running sums.
+template <int kN, int POWER>
+__device__ __forceinline__ void add(Sums &s, const float *z, float c_tau) {
+    float top = s.top;
+#pragma unroll
+    for (int k = 0; k < kN; ++k) top = fmaxf(top, z[k]);
+    const float ref = against(top);
+    if (top > s.top) {
+        s.tau *= exp2_of((s.top - ref) * c_tau);
+        s.one *= exp2_of((s.top - ref) * kLog2e);
+        s.top = top;
+    }
+    add_against<kN, POWER>(s, z, ref, c_tau);
+}
+
+// The sums and terms of part blockIdx.y of row blockIdx.x.
+template <typename T, int POWER>
+__global__ __launch_bounds__(kSplitThreads) void k_distill_sums(DistillArgs a) {
+    constexpr int kN = kPer<T>;
+    __shared__ Sums waves[kSplitThreads / 64];
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x;
     const T *z = (const T *)a.logits + row * a.logit_stride;
-    const int K = a.k;
-
-    // the teacher's softmax over the entries that are there
-    float top = kNegInf, bad = 0.0f;
-    for (int j = tid; j < K; j += kThreads) {
-        const int64_t idx = load_int(a.teacher_index, row * K + j, a.index64);
-        const bool there = idx >= 0;
-        if (there && idx >= a.vocab) bad = 1.0f;
-        t.index[j] = there && idx < a.vocab ? (int)idx : -1;
-        t.q[j] = there ? load_either(a.teacher_logits, row * K + j, a.teacher_bf16) * a.inv_tau : kNegInf;
-        top = fmaxf(top, t.q[j]);
-    }
-    top = block_reduce<false>(top, scratch);
-    bad = block_reduce<false>(bad, scratch);
-    float sum = 0.0f;
-    const float ref = top == kNegInf ? 0.0f : top;
-    for (int j = tid; j < K; j += kThreads) sum += exp_of(t.q[j] - ref);
-    sum = block_reduce<true>(sum, scratch);
-    const float log_sum = logf(sum) + ref;
-    const bool has_teacher = a.distill_weight != 0.0f && (top != kNegInf || sum != 0.0f);
-    int64_t label = a.labels && a.label_weight != 0.0f ? load_int(a.labels, row, a.index64) : -1;
-    if (label >= a.vocab) bad = 1.0f, label = -1;
-    const bool has_label = label >= 0;
-    for (int j = tid; j < K; j += kThreads) {
-        t.log_q[j] = t.q[j] - log_sum;
-        t.q[j] = t.q[j] == kNegInf ? 0.0f : exp_of(t.log_q[j]);
-        t.z[j] = t.index[j] >= 0 ? load1(z + t.index[j]) : 0.0f;
-    }
-    const float z_label = has_label ? load1(z + label) : 0.0f;
-
-    float l_tau, l_one;
-    if (BACK) {
-        l_tau = a.lse_in[2 * row];
-        l_one = a.lse_in[2 * row + 1];
-    } else {
-        Stats st = nothing();
-        for (int64_t v = tid; v < a.vocab; v += kThreads) add(st, load1(z + v), a.inv_tau);
-        for (int d = 32; d > 0; d >>= 1)
-            st = join(st, {__shfl_xor(st.top, d), __shfl_xor(st.s_tau, d), __shfl_xor(st.s_one, d)}, a.inv_tau);
-        if ((tid & 63) == 0) waves[tid >> 6] = st;
-        __syncthreads();
-        st = waves[0];
-        for (int w = 1; w < kThreads / 64; ++w) st = join(st, waves[w], a.inv_tau);
-        l_tau = logf(st.s_tau) + st.top * a.inv_tau;
-        l_one = logf(st.s_one) + st.top;
-        float kl = 0.0f;
-        for (int j = tid; j < K; j += kThreads)
-            if (t.q[j] > 0.0f || t.q[j] != t.q[j])
-                kl += t.q[j] * (t.log_q[j] - (t.z[j] * a.inv_tau - l_tau));
-        kl = block_reduce<true>(kl, scratch);
-        if (tid == 0) {
-            float loss = 0.0f;
-            if (has_teacher) loss = a.distill_weight * a.tau * a.tau * kl;
-            if (has_label) loss += a.label_weight * (l_one - z_label);
-            a.loss[row] = bad != 0.0f ? __builtin_nanf("") : loss;
-            if (a.lse) {
-                a.lse[2 * row] = l_tau;
-                a.lse[2 * row + 1] = l_one;
-            }
+    const Part p = part_of<T>(a, blockIdx.y, a.splits);
+    const float c_tau = a.inv_tau * kLog2e;
+    Sums s{kNegInf, 0.0f, 0.0f};
+    for (int64_t i = p.p0 + tid; i < p.p1; i += kSplitThreads * kSplitAhead) {
+        u32x4 r[kSplitAhead];
+#pragma unroll
+        for (int u = 0; u < kSplitAhead; ++u)
+            r[u] = i + u * kSplitThreads < p.p1 ? load_piece(z + (i + u * kSplitThreads) * kN) : nothing<T>();
+#pragma unroll
+        for (int u = 0; u < kSplitAhead; ++u) {
+            float v[kN];
+            floats_of(r[u], z, v);
+            add<kN, POWER>(s, v, c_tau);
         }
     }
-    if (!a.dlogits) return;
+    const int64_t rest = p.p1 * kN + tid;
+    if (rest < p.v1) {
+        const float v = load1(z + rest);
+        add<1, POWER>(s, &v, c_tau);
+    }
+    if (POWER == 0) s.one = s.tau;
+    s = wave_join(s, c_tau);
+    if ((tid & 63) == 0) waves[tid >> 6] = s;
+    __syncthreads();
+    if (tid >= 64) return;
+    s = waves[0];
+#pragma unroll
+    for (int w = 1; w < kSplitThreads / 64; ++w) s = join(s, waves[w], c_tau);
+    const Row r = row_of(a, row);
+    const Terms t = wave_terms(a, row, r, z_at<T>, z, p.v0, p.v1);
+    if (tid == 0) {
+        float *out = a.partials + (row * a.splits + blockIdx.y) * kDistillPartials;
+        out[0] = s.top, out[1] = s.tau, out[2] = s.one;
+        out[3] = t.dot, out[4] = t.q, out[5] = t.z_label;
+    }
+}
 
-    // the gradient: every z_j is in LDS, so dlogits may be logits itself
+// The parts of a row joined, by one whole wave.
+__device__ void join_parts(const DistillArgs &a, int64_t row, Sums *s, Terms *t) {
+    const float c_tau = a.inv_tau * kLog2e;
+    *s = Sums{kNegInf, 0.0f, 0.0f};
+    *t = Terms{0.0f, 0.0f, 0.0f};
+    for (int i = threadIdx.x & 63; i < a.splits; i += 64) {
+        const float *p = a.partials + (row * a.splits + i) * kDistillPartials;
+        *s = join(*s, {p[0], p[1], p[2]}, c_tau);
+        t->dot += p[3], t->q += p[4], t->z_label += p[5];
+    }
+    *s = wave_join(*s, c_tau);
+    t->dot = wave_sum(t->dot), t->q = wave_sum(t->q), t->z_label = wave_sum(t->z_label);
+}
+
+__device__ void write_loss(const DistillArgs &a, int64_t row, const Row &r, const Sums &s, const Terms &t) {
+    const float l_tau = log_of(s.tau, s.top, a.inv_tau), l_one = log_of(s.one, s.top, 1.0f);
+    a.loss[row] = loss_of(a, r, t, l_tau, l_one);
+    if (a.lse) {
+        a.lse[2 * row] = l_tau;
+        a.lse[2 * row + 1] = l_one;
+    }
+}
+
+// The loss alone: a wave joins a row's parts.
+__global__ __launch_bounds__(64) void k_distill_loss(DistillArgs a) {
+    const int64_t row = blockIdx.x;
+    const Row r = row_of(a, row);
+    Sums s;
+    Terms t;
+    join_parts(a, row, &s, &t);
+    if (threadIdx.x == 0) write_loss(a, row, r, s, t);
+}
+
+// The gradient of part blockIdx.y of row blockIdx.x, from the joined parts (and
+// the loss, by part 0) or, backward, from lse.
+template <typename T, int POWER, bool BACK>
+__global__ __launch_bounds__(kSplitThreads) void k_distill_gradient(DistillArgs a) {
+    constexpr int kN = kPer<T>;
+    __shared__ Entries entries;
+    __shared__ Slope shared_slope;
+    __shared__ Row shared_row;
+    const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x;
+    const T *z = (const T *)a.logits + row * a.logit_stride;
     T *dz = (T *)a.dlogits + row * a.dlogits_stride;
-    const float g = bad != 0.0f ? __builtin_nanf("") : a.row_grad[row];
-    const float c_tau = has_teacher || bad != 0.0f ? g * a.distill_weight * a.tau : 0.0f;
-    const float c_one = has_label || bad != 0.0f ? g * a.label_weight : 0.0f;
-    auto plain = [&](float x) {
-        float d = 0.0f;
-        if (c_tau != 0.0f) d = c_tau * exp_of(x * a.inv_tau - l_tau);
-        if (c_one != 0.0f) d += c_one * exp_of(x - l_one);
-        return d;
-    };
-    __syncthreads();
-    for (int64_t v = tid; v < a.vocab; v += kThreads) store1(dz + v, plain(load1(z + v)));
-    __syncthreads();
-    // the elements that the teacher or the label names, over what the walk wrote
-    for (int j = tid; j < K + 1; j += kThreads) {
-        const int64_t at = j < K ? t.index[j] : label;
-        if (at < 0) continue;
-        float d = plain(j < K ? t.z[j] : z_label);
-        if (c_tau != 0.0f) {
-            float q = 0.0f;
-            for (int i = 0; i < K; ++i) q += t.index[i] == (int)at ? t.q[i] : 0.0f;
-            d -= c_tau * q;
+    const Part p = part_of<T>(a, blockIdx.y, a.parts);
+    if (tid < 64) {
+        const Row r = row_of(a, row);
+        const float g = a.row_grad[row];
+        Slope d;
+        if (BACK) {
+            d = slope_of<POWER, true>(a, r, g, {}, a.lse_in[2 * row], a.lse_in[2 * row + 1]);
+        } else {
+            Sums s;
+            Terms t;
+            join_parts(a, row, &s, &t);
+            d = slope_of<POWER, false>(a, r, g, s, 0.0f, 0.0f);
+            if (blockIdx.y == 0 && tid == 0) write_loss(a, row, r, s, t);
         }
-        if (at == label) d -= c_one;
-        store1(dz + at, d);
+        gather_entries(a, row, r, z, p.v0, p.v1, entries);
+        if (tid == 0) shared_slope = d, shared_row = r;
     }
+    __syncthreads();
+    const Slope d = shared_slope;
+    const Row r = shared_row;
+    if (d.k_tau == 0.0f && d.k_one == 0.0f) {
+        // nothing here is learned from: zeros, whatever the logits hold
+        const float zero[kN] = {};
+        for (int64_t i = p.p0 + tid; i < p.p1; i += kSplitThreads) store_piece(dz + i * kN, zero);
+        if (p.p1 * kN + tid < p.v1) store1(dz + p.p1 * kN + tid, 0.0f);
+        return;
+    }
+    for (int64_t i = p.p0 + tid; i < p.p1; i += kSplitThreads * kSplitAhead) {
+        u32x4 raw[kSplitAhead];
+#pragma unroll
+        for (int u = 0; u < kSplitAhead; ++u)
+            raw[u] = i + u * kSplitThreads < p.p1 ? load_piece(z + (i + u * kSplitThreads) * kN) : nothing<T>();
+#pragma unroll
+        for (int u = 0; u < kSplitAhead; ++u) {
+            if (i + u * kSplitThreads >= p.p1) break;
+            float v[kN];
+            floats_of(raw[u], z, v);
+#pragma unroll
+            for (int k = 0; k < kN; ++k) v[k] = slope_at<POWER, BACK>(d, v[k]);
+            store_piece(dz + (i + u * kSplitThreads) * kN, v);
+        }
+    }
+    const int64_t rest = p.p1 * kN + tid;
+    if (rest < p.v1) store1(dz + rest, slope_at<POWER, BACK>(d, load1(z + rest)));
+    __syncthreads();
+    correct_entries<T, POWER, BACK>(a, r, d, entries, dz);
+}
+
+// ---- resident rows ------------------------------------------------------------------------
+
+// The largest of 8 BF16 values at a time as 16-bit integers: right if it is not
+// negative, as then the order of the bits is that of the values (a NaN with its
+// sign clear comes out largest, and makes the sums NaN as it should).
+typedef __attribute__((ext_vector_type(8))) short s16x8;
+__device__ __forceinline__ s16x8 top_bits(s16x8 m, u32x4 r) {
+    return __builtin_elementwise_max(m, __builtin_bit_cast(s16x8, r));
+}
+__device__ __forceinline__ float top_of_bits(s16x8 m) {
+    short t = m[0];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) t = t > m[k] ? t : m[k];
+    return t >= 0 ? __uint_as_float((uint32_t)t << 16) : kNegInf;
+}
+
+// A block of THREADS holds a row in up to NV 16-byte pieces a thread.  SUMS and
+// POWER: the sums' and the gradient's.
+template <typename T, int THREADS, int NV, int SUMS, int POWER>
+__global__ __launch_bounds__(THREADS) void k_distill_resident(DistillArgs a) {
+    constexpr int kN = kPer<T>, kWaves = THREADS / 64;
+    __shared__ Entries entries;
+    __shared__ float red[3][kWaves];
+    __shared__ Row shared_row;
+    __shared__ Terms shared_terms;
+    const int tid = threadIdx.x, wave = tid >> 6;
+    const int pieces = a.vocab / kN, rest = pieces * kN + tid;
+    const float c_tau = a.inv_tau * kLog2e;
+    const T *const type = nullptr;
+    u32x4 held[NV];
+    float last = kNegInf;
+    int64_t row = blockIdx.x;
+    // a thread's pieces are THREADS apart: one offset, and a scalar base for each
+    const uint32_t at = (uint32_t)tid * kN;
+    {
+        const T *z = (const T *)a.logits + row * a.logit_stride;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+            held[j] = tid + j * THREADS < pieces ? load_piece_once(z + j * THREADS * kN + at) : nothing<T>();
+        if (rest < a.vocab) last = load1(z + rest);
+    }
+    for (; row < a.rows; row += gridDim.x) {
+        const T *z = (const T *)a.logits + row * a.logit_stride;
+        if (tid < 64) {
+            const Row r = row_of(a, row);
+            gather_entries(a, row, r, z, 0, a.vocab, entries);
+            const Terms t = wave_terms(a, row, r, z_at<T>, z, 0, a.vocab);
+            if (tid == 0) shared_row = r, shared_terms = t;
+        }
+        // the block's largest of v
+        auto block_top = [&](float v) __attribute__((always_inline)) {
+            v = wave_max(v);
+            __syncthreads();
+            if ((tid & 63) == 0) red[0][wave] = v;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) v = fmaxf(v, red[0][w]);
+            return v;
+        };
+        float top = kNegInf;
+        if constexpr (kN == 8) {
+            s16x8 m = (short)-32768;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) m = top_bits(m, held[j]);
+            const float t = top_of_bits(m);
+            top = block_top(t != t || !(last >= t) ? t : last);
+        }
+        if (kN != 8 || top == kNegInf) {
+            // 32 bits, or nothing in the row but negative values
+            top = last;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                float v[kN];
+                floats_of(held[j], type, v);
+#pragma unroll
+                for (int k = 0; k < kN; ++k) top = fmaxf(top, v[k]);
+                forget(held[j]);
+            }
+            top = block_top(top);
+        }
+        const float ref = against(top);
+        Sums mine{top, 0.0f, 0.0f};
+        add_against<1, SUMS>(mine, &last, ref, c_tau);
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            float v[kN];
+            floats_of(held[j], type, v);
+            add_against<kN, SUMS>(mine, v, ref, c_tau);
+            forget(held[j]);
+        }
+        const float s_tau = wave_sum(mine.tau), s_one = SUMS ? wave_sum(mine.one) : 0.0f;
+        if ((tid & 63) == 0) red[1][wave] = s_tau, red[2][wave] = s_one;
+        __syncthreads();
+        Sums s{top, 0.0f, 0.0f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) s.tau += red[1][w], s.one += red[2][w];
+        if (!SUMS) s.one = s.tau;
+        const Row r = shared_row;
+        if (tid == 0) write_loss(a, row, r, s, shared_terms);
+        const Slope d = slope_of<POWER, false>(a, r, a.row_grad[row], s, 0.0f, 0.0f);
+        const bool zeros = d.k_tau == 0.0f && d.k_one == 0.0f;
+
+        T *dz = (T *)a.dlogits + row * a.dlogits_stride;
+        const int64_t next = row + gridDim.x;
+        const T *zn = (const T *)a.logits + (next < a.rows ? next : row) * a.logit_stride;
+        const int pieces_next = next < a.rows ? pieces : 0;
+        if (rest < a.vocab) store1(dz + rest, zeros ? 0.0f : slope_at<POWER, false>(d, last));
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            const int i = tid + j * THREADS;
+            float v[kN];
+            floats_of(held[j], type, v);
+#pragma unroll
+            for (int k = 0; k < kN; ++k) v[k] = zeros ? 0.0f : slope_at<POWER, false>(d, v[k]);
+            if (i < pieces) store_piece(dz + j * THREADS * kN + at, v);
+            // its register takes the next row's piece
+            held[j] = i < pieces_next ? load_piece_once(zn + j * THREADS * kN + at) : nothing<T>();
+        }
+        last = rest < a.vocab && next < a.rows ? load1(zn + rest) : kNegInf;
+        __syncthreads();
+        if (!zeros) correct_entries<T, POWER, false>(a, r, d, entries, dz);
+        __syncthreads();
+    }
+}
+
+// POWER of the sums (both are wanted: lse holds both), and of the gradient.
+int sums_power(const DistillArgs &a) {
+    if (a.tau == 1.0f) return 0;
+    return a.tau == 2.0f ? 2 : a.tau == 3.0f ? 3 : a.tau == 4.0f ? 4 : 1;
+}
+int gradient_power(const DistillArgs &a) {
+    return a.distill_weight != 0.0f && a.label_weight != 0.0f && a.labels ? sums_power(a) : 0;
+}
+
+template <typename T, int THREADS, int NV>
+void launch_resident(const DistillArgs &a, int per_cu, hipStream_t s) {
+    const dim3 grid((uint32_t)std::min<int64_t>(a.rows, 256 * per_cu));
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(THREADS), 0, s, a); };
+    switch (gradient_power(a)) {
+        case 1: return go(k_distill_resident<T, THREADS, NV, 1, 1>);
+        case 2: return go(k_distill_resident<T, THREADS, NV, 2, 2>);
+        case 3: return go(k_distill_resident<T, THREADS, NV, 3, 3>);
+        case 4: return go(k_distill_resident<T, THREADS, NV, 4, 4>);
+        default: break;
+    }
+    if (sums_power(a) == 0)
+        go(k_distill_resident<T, THREADS, NV, 0, 0>);
+    else
+        go(k_distill_resident<T, THREADS, NV, 1, 0>);
+}
+
+// 16-byte pieces of a row.
+int64_t pieces_of(const DistillArgs &a, bool bf16) { return a.vocab / (bf16 ? 8 : 4); }
+
+// Whether rows stay in registers: a gradient is wanted, a row fits a compute
+// unit's, and there are rows enough to give most units one.
+bool resident(const DistillArgs &a, bool bf16) {
+    return a.dlogits && pieces_of(a, bf16) <= 20 * 1024 && a.rows >= 192;
+}
+
+template <typename T>
+void launch_resident_any(const DistillArgs &a, hipStream_t s) {
+    const int64_t n = pieces_of(a, sizeof(T) == 2);
+    if (n <= 4 * 256) return launch_resident<T, 256, 4>(a, 6, s);
+    if (n <= 8 * 256) return launch_resident<T, 256, 8>(a, 6, s);
+    if (n <= 16 * 256) return launch_resident<T, 256, 16>(a, 4, s);
+    if (n <= 8 * 1024) return launch_resident<T, 1024, 8>(a, 2, s);
+    if (n <= 12 * 1024) return launch_resident<T, 1024, 12>(a, 1, s);
+    if (n <= 16 * 1024) return launch_resident<T, 1024, 16>(a, 1, s);
+    return launch_resident<T, 1024, 20>(a, 1, s);
+}
+
+// Parts of a row so that the grid fills the compute units several times, none
+// smaller than a block's loads.
+int parts_of(const DistillArgs &a, bool bf16) {
+    const int64_t want = (2048 + a.rows - 1) / std::max<int64_t>(1, a.rows);
+    const int64_t most = std::max<int64_t>(1, pieces_of(a, bf16) / (kSplitThreads * kSplitAhead));
+    return (int)std::max<int64_t>(1, std::min<int64_t>({want, most, 64}));
+}
+
+template <typename T, bool BACK>
+void launch_gradient(const DistillArgs &a, hipStream_t s) {
+    const dim3 grid((uint32_t)a.rows, a.parts);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kSplitThreads), 0, s, a); };
+    switch (gradient_power(a)) {
+        case 0: return go(k_distill_gradient<T, 0, BACK>);
+        case 2: return go(k_distill_gradient<T, 2, BACK>);
+        case 3: return go(k_distill_gradient<T, 3, BACK>);
+        case 4: return go(k_distill_gradient<T, 4, BACK>);
+        default: return go(k_distill_gradient<T, 1, BACK>);
+    }
+}
+
+template <typename T>
+hipError_t launch_forward(const DistillArgs &a, hipStream_t s) {
+    if (a.splits == 0) {
+        launch_resident_any<T>(a, s);
+        return hipGetLastError();
+    }
+    const dim3 grid((uint32_t)a.rows, a.splits);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kSplitThreads), 0, s, a); };
+    switch (sums_power(a)) {
+        case 0: go(k_distill_sums<T, 0>); break;
+        case 2: go(k_distill_sums<T, 2>); break;
+        case 3: go(k_distill_sums<T, 3>); break;
+        case 4: go(k_distill_sums<T, 4>); break;
+        default: go(k_distill_sums<T, 1>); break;
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (a.dlogits)
+        launch_gradient<T, false>(a, s);
+    else
+        hipLaunchKernelGGL(k_distill_loss, dim3((uint32_t)a.rows), dim3(64), 0, s, a);
+    return hipGetLastError();
 }
 
 }  // namespace
 
-int distill_splits(const DistillArgs &, bool) { return 1; }
+int distill_splits(const DistillArgs &a, bool bf16) { return resident(a, bf16) ? 0 : parts_of(a, bf16); }
 
-hipError_t launch_distill(const DistillArgs &a, bool bf16, hipStream_t s) {
-    if (a.rows == 0) return hipSuccess;
-    if (bf16)
-        hipLaunchKernelGGL((k_distill_rows<uint16_t, false>), dim3((uint32_t)a.rows), dim3(kThreads), 0, s, a);
-    else
-        hipLaunchKernelGGL((k_distill_rows<float, false>), dim3((uint32_t)a.rows), dim3(kThreads), 0, s, a);
-    return hipGetLastError();
+hipError_t launch_distill(const DistillArgs &args, bool bf16, hipStream_t s) {
+    if (args.rows == 0) return hipSuccess;
+    DistillArgs a = args;
+    a.parts = parts_of(a, bf16);
+    return bf16 ? launch_forward<uint16_t>(a, s) : launch_forward<float>(a, s);
 }
 
-hipError_t launch_distill_backward(const DistillArgs &a, bool bf16, hipStream_t s) {
-    if (a.rows == 0) return hipSuccess;
-    if (bf16)
-        hipLaunchKernelGGL((k_distill_rows<uint16_t, true>), dim3((uint32_t)a.rows), dim3(kThreads), 0, s, a);
-    else
-        hipLaunchKernelGGL((k_distill_rows<float, true>), dim3((uint32_t)a.rows), dim3(kThreads), 0, s, a);
+hipError_t launch_distill_backward(const DistillArgs &args, bool bf16, hipStream_t s) {
+    if (args.rows == 0) return hipSuccess;
+    DistillArgs a = args;
+    // parts of about 16 KB and more
+    a.parts = (int)std::max<int64_t>(parts_of(a, bf16), std::min<int64_t>(8, pieces_of(a, bf16) / (2 * kSplitThreads * kSplitAhead)));
+    bf16 ? launch_gradient<uint16_t, true>(a, s) : launch_gradient<float, true>(a, s);
     return hipGetLastError();
 }
 

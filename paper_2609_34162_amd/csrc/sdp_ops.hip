@@ -333,13 +333,14 @@ int distill_call(sdp_ctx *ctx, const char *call, const sdp_distill_desc *d, floa
         return SDP_OK;
     }
     a.splits = sdpops::distill_splits(a, bf16);
-    if (a.splits > 1) {
-        SDP_TRY(ensure_ops_space(ctx, (size_t)rows * a.splits * 16));
+    const bool parts = a.splits > 0 && rows > 0;
+    if (parts) {
+        SDP_TRY(ensure_ops_space(ctx, (size_t)rows * a.splits * sdpops::kDistillPartials * sizeof(float)));
         a.partials = (float *)ctx->ops_space;
         SDP_TRY(ops_order(ctx, s));
     }
     HIP_TRY(sdpops::launch_distill(a, bf16, s));
-    if (a.splits > 1) SDP_TRY(ops_mark(ctx, s));
+    if (parts) SDP_TRY(ops_mark(ctx, s));
     return SDP_OK;
 }
 

@@ -82,11 +82,14 @@ struct DistillArgs {
     const float *row_grad;
     void *dlogits;                 // NULL: loss only
     int64_t dlogits_stride;
-    float *partials;               // rows split over blocks: [rows, splits, 4]
-    int32_t splits;
+    float *partials;               // [rows, splits, kDistillPartials]: what each part of a row found
+    int32_t splits;                // parts of a row for its sums; 0: rows stay in registers
+    int32_t parts;                 // and for its gradient
 };
 
-// How many blocks share a row (1: none split).
+constexpr int kDistillPartials = 8;
+
+// The parts of a row for its sums, or 0 where the call takes no partials.
 int distill_splits(const DistillArgs &a, bool bf16);
 hipError_t launch_distill(const DistillArgs &a, bool bf16, hipStream_t s);
 hipError_t launch_distill_backward(const DistillArgs &a, bool bf16, hipStream_t s);
