@@ -145,7 +145,6 @@ __device__ Row row_of(const DistillArgs &a, int64_t row) {
     if (label >= a.vocab) bad = 1.0f, label = -1;
     r.label = (int32_t)label;
     r.has_label = label >= 0;
-    if (label < 0) r.label = -1;
     r.bad = wave_max(bad) != 0.0f;
     return r;
 }
@@ -165,8 +164,8 @@ struct Terms {
     float dot, q, z_label;
 };
 
-__device__ Terms wave_terms(const DistillArgs &a, int64_t row, const Row &r, float (*z_at)(const void *, int64_t),
-                            const void *z, int64_t v0, int64_t v1) {
+template <typename T>
+__device__ Terms wave_terms(const DistillArgs &a, int64_t row, const Row &r, const T *z, int64_t v0, int64_t v1) {
     const int lane = threadIdx.x & 63;
     Terms t{0.0f, 0.0f, 0.0f};
     if (r.has_teacher)
@@ -174,18 +173,13 @@ __device__ Terms wave_terms(const DistillArgs &a, int64_t row, const Row &r, flo
             float q, log_q;
             const int32_t v = entry(a, row, r, j, &q, &log_q);
             if (v < v0 || v >= v1 || q == 0.0f) continue;
-            t.dot += q * (log_q - z_at(z, v) * a.inv_tau);
+            t.dot += q * (log_q - load1(z + v) * a.inv_tau);
             t.q += q;
         }
     t.dot = wave_sum(t.dot);
     t.q = wave_sum(t.q);
-    if (r.label >= v0 && r.label < v1) t.z_label = z_at(z, r.label);
+    if (r.label >= v0 && r.label < v1) t.z_label = load1(z + r.label);
     return t;
-}
-
-template <typename T>
-__device__ float z_at(const void *z, int64_t v) {
-    return load1((const T *)z + v);
 }
 
 __device__ float loss_of(const DistillArgs &a, const Row &r, const Terms &t, float l_tau, float l_one) {
@@ -322,7 +316,8 @@ __device__ __forceinline__ void add(Sums &s, const float *z, float c_tau) {
     add_against<kN, POWER>(s, z, ref, c_tau);
 }
 
-// The sums and terms of part blockIdx.y of row blockIdx.x.
+// The sums of part blockIdx.y of row blockIdx.x and, where a gradient follows (it
+// may overwrite the logits), what the part says to the loss.
 template <typename T, int POWER>
 __global__ __launch_bounds__(kSplitThreads) void k_distill_sums(DistillArgs a) {
     constexpr int kN = kPer<T>;
@@ -358,8 +353,8 @@ __global__ __launch_bounds__(kSplitThreads) void k_distill_sums(DistillArgs a) {
     s = waves[0];
 #pragma unroll
     for (int w = 1; w < kSplitThreads / 64; ++w) s = join(s, waves[w], c_tau);
-    const Row r = row_of(a, row);
-    const Terms t = wave_terms(a, row, r, z_at<T>, z, p.v0, p.v1);
+    Terms t{0.0f, 0.0f, 0.0f};
+    if (a.dlogits) t = wave_terms<T>(a, row, row_of(a, row), z, p.v0, p.v1);
     if (tid == 0) {
         float *out = a.partials + (row * a.splits + blockIdx.y) * kDistillPartials;
         out[0] = s.top, out[1] = s.tau, out[2] = s.one;
@@ -391,12 +386,14 @@ __device__ void write_loss(const DistillArgs &a, int64_t row, const Row &r, cons
 }
 
 // The loss alone: a wave joins a row's parts.
+template <typename T>
 __global__ __launch_bounds__(64) void k_distill_loss(DistillArgs a) {
     const int64_t row = blockIdx.x;
     const Row r = row_of(a, row);
     Sums s;
     Terms t;
     join_parts(a, row, &s, &t);
+    t = wave_terms<T>(a, row, r, (const T *)a.logits + row * a.logit_stride, 0, a.vocab);
     if (threadIdx.x == 0) write_loss(a, row, r, s, t);
 }
 
@@ -481,51 +478,90 @@ __device__ __forceinline__ float top_of_bits(s16x8 m) {
 template <typename T, int THREADS, int NV, int SUMS, int POWER>
 __global__ __launch_bounds__(THREADS) void k_distill_resident(DistillArgs a) {
     constexpr int kN = kPer<T>, kWaves = THREADS / 64;
-    __shared__ Entries entries;
-    __shared__ float red[3][kWaves];
-    __shared__ Row shared_row;
-    __shared__ Terms shared_terms;
+    // the entries (q: t / tau at first, then q times t_sum) of this row and the next;
+    // entry j, and the label as entry k, belong to thread j mod THREADS
+    __shared__ Entries both[2];
+    __shared__ float red[4][kWaves];
+    __shared__ int bad_waves[kWaves];
     const int tid = threadIdx.x, wave = tid >> 6;
     const int pieces = a.vocab / kN, rest = pieces * kN + tid;
     const float c_tau = a.inv_tau * kLog2e;
+    const bool labels = a.labels && a.label_weight != 0.0f, teacher = a.distill_weight != 0.0f;
     const T *const type = nullptr;
     u32x4 held[NV];
     float last = kNegInf;
     int64_t row = blockIdx.x;
     // a thread's pieces are THREADS apart: one offset, and a scalar base for each
     const uint32_t at = (uint32_t)tid * kN;
+    // places and t / tau of a row's entries; an index past the vocabulary is kept as its size
+    auto fetch_entries = [&](int64_t of, Entries &en) __attribute__((always_inline)) {
+#pragma unroll 1
+        for (int j = tid; j <= a.k; j += THREADS) {
+            int64_t v = -1;
+            float t = kNegInf;
+            if (j < a.k) {
+                v = load_int(a.teacher_index, of * a.k + j, a.index64);
+                t = load_either(a.teacher_logits, of * a.k + j, a.teacher_bf16) * a.inv_tau;
+            } else if (labels) {
+                v = load_int(a.labels, of, a.index64);
+            }
+            en.index[j] = v < 0 ? -1 : v < a.vocab ? (int32_t)v : a.vocab;
+            en.q[j] = v < 0 ? kNegInf : t;
+        }
+    };
+    // and their logits, from the same thread
+    auto fetch_logits = [&](const T *z, Entries &en) __attribute__((always_inline)) {
+#pragma unroll 1
+        for (int j = tid; j <= a.k; j += THREADS) {
+            const int32_t v = en.index[j];
+            en.z[j] = v >= 0 && v < a.vocab ? load1(z + v) : 0.0f;
+        }
+    };
     {
         const T *z = (const T *)a.logits + row * a.logit_stride;
+        fetch_entries(row, both[0]);
 #pragma unroll
         for (int j = 0; j < NV; ++j)
             held[j] = tid + j * THREADS < pieces ? load_piece_once(z + j * THREADS * kN + at) : nothing<T>();
         if (rest < a.vocab) last = load1(z + rest);
+        fetch_logits(z, both[0]);
     }
-    for (; row < a.rows; row += gridDim.x) {
-        const T *z = (const T *)a.logits + row * a.logit_stride;
-        if (tid < 64) {
-            const Row r = row_of(a, row);
-            gather_entries(a, row, r, z, 0, a.vocab, entries);
-            const Terms t = wave_terms(a, row, r, z_at<T>, z, 0, a.vocab);
-            if (tid == 0) shared_row = r, shared_terms = t;
-        }
-        // the block's largest of v
-        auto block_top = [&](float v) __attribute__((always_inline)) {
-            v = wave_max(v);
-            __syncthreads();
-            if ((tid & 63) == 0) red[0][wave] = v;
-            __syncthreads();
+    // over the block's threads: the largest x, and y
+    auto block_top = [&](float x, float y, float *y_top) __attribute__((always_inline)) {
+        x = wave_max(x), y = wave_max(y);
+        __syncthreads();
+        if ((tid & 63) == 0) red[0][wave] = x, red[1][wave] = y;
+        __syncthreads();
+        x = red[0][tid & (kWaves - 1)], y = red[1][tid & (kWaves - 1)];
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) v = fmaxf(v, red[0][w]);
-            return v;
-        };
+        for (int w = 1; w < kWaves; w <<= 1) x = fmaxf(x, __shfl_xor(x, w)), y = fmaxf(y, __shfl_xor(y, w));
+        *y_top = y;
+        return x;
+    };
+    auto block_sum = [&](const float *of) __attribute__((always_inline)) {
+        float x = of[tid & (kWaves - 1)];
+#pragma unroll
+        for (int w = 1; w < kWaves; w <<= 1) x += __shfl_xor(x, w);
+        return x;
+    };
+    for (int parity = 0; row < a.rows; row += gridDim.x, parity ^= 1) {
+        Entries &entries = both[parity], &entries_next = both[parity ^ 1];
+        float t_top = kNegInf;
+        bool bad = false;
+#pragma unroll 1
+        for (int j = tid; j <= a.k; j += THREADS) {
+            t_top = fmaxf(t_top, entries.q[j]);
+            bad = bad || entries.index[j] == a.vocab;
+        }
+        const bool wave_bad = __any(bad);
+        if ((tid & 63) == 0) bad_waves[wave] = wave_bad;
         float top = kNegInf;
         if constexpr (kN == 8) {
             s16x8 m = (short)-32768;
 #pragma unroll
             for (int j = 0; j < NV; ++j) m = top_bits(m, held[j]);
-            const float t = top_of_bits(m);
-            top = block_top(t != t || !(last >= t) ? t : last);
+            const float own = top_of_bits(m);
+            top = block_top(own != own || !(last >= own) ? own : last, t_top, &t_top);
         }
         if (kN != 8 || top == kNegInf) {
             // 32 bits, or nothing in the row but negative values
@@ -538,9 +574,20 @@ __global__ __launch_bounds__(THREADS) void k_distill_resident(DistillArgs a) {
                 for (int k = 0; k < kN; ++k) top = fmaxf(top, v[k]);
                 forget(held[j]);
             }
-            top = block_top(top);
+            top = block_top(top, t_top, &t_top);
         }
-        const float ref = against(top);
+        const float ref = against(top), t_ref = against(t_top);
+        // the teacher's sum of exp(t / tau - top), and of that times t / tau - top - z / tau
+        float t_sum = 0.0f, t_dot = 0.0f;
+#pragma unroll 1
+        for (int j = tid; j <= a.k; j += THREADS) {
+            const float t = entries.q[j];
+            const float q = t != kNegInf ? exp2_of((t - t_ref) * kLog2e) : 0.0f;
+            t_sum += q;
+            if (q != 0.0f) t_dot += q * (t - t_ref - entries.z[j] * a.inv_tau);
+            entries.q[j] = q;
+            if (entries.index[j] == a.vocab) entries.index[j] = -1;
+        }
         Sums mine{top, 0.0f, 0.0f};
         add_against<1, SUMS>(mine, &last, ref, c_tau);
 #pragma unroll
@@ -550,22 +597,32 @@ __global__ __launch_bounds__(THREADS) void k_distill_resident(DistillArgs a) {
             add_against<kN, SUMS>(mine, v, ref, c_tau);
             forget(held[j]);
         }
-        const float s_tau = wave_sum(mine.tau), s_one = SUMS ? wave_sum(mine.one) : 0.0f;
-        if ((tid & 63) == 0) red[1][wave] = s_tau, red[2][wave] = s_one;
+        const float w_tau = wave_sum(mine.tau), w_one = SUMS ? wave_sum(mine.one) : 0.0f;
+        t_sum = wave_sum(t_sum), t_dot = wave_sum(t_dot);
         __syncthreads();
-        Sums s{top, 0.0f, 0.0f};
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) s.tau += red[1][w], s.one += red[2][w];
+        if ((tid & 63) == 0) red[0][wave] = w_tau, red[1][wave] = w_one, red[2][wave] = t_sum, red[3][wave] = t_dot;
+        __syncthreads();
+        Sums s{top, block_sum(red[0]), SUMS ? block_sum(red[1]) : 0.0f};
+        t_sum = block_sum(red[2]), t_dot = block_sum(red[3]);
+        Row r;
+        r.bad = __any(bad_waves[tid & (kWaves - 1)]);
         if (!SUMS) s.one = s.tau;
-        const Row r = shared_row;
-        if (tid == 0) write_loss(a, row, r, s, shared_terms);
-        const Slope d = slope_of<POWER, false>(a, r, a.row_grad[row], s, 0.0f, 0.0f);
+        r.has_teacher = teacher && (t_top != kNegInf || t_sum != 0.0f);
+        r.label = labels ? entries.index[a.k] : -1;
+        r.has_label = r.label >= 0;
+        if (tid == 0) {
+            // sum of q (log q - z / tau), the q's sum being 1
+            Terms terms{t_dot / t_sum - logf(t_sum), 1.0f, entries.z[a.k]};
+            write_loss(a, row, r, s, terms);
+        }
+        Slope d = slope_of<POWER, false>(a, r, a.row_grad[row], s, 0.0f, 0.0f);
         const bool zeros = d.k_tau == 0.0f && d.k_one == 0.0f;
 
         T *dz = (T *)a.dlogits + row * a.dlogits_stride;
         const int64_t next = row + gridDim.x;
         const T *zn = (const T *)a.logits + (next < a.rows ? next : row) * a.logit_stride;
         const int pieces_next = next < a.rows ? pieces : 0;
+        if (next < a.rows) fetch_entries(next, entries_next);
         if (rest < a.vocab) store1(dz + rest, zeros ? 0.0f : slope_at<POWER, false>(d, last));
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -579,7 +636,10 @@ __global__ __launch_bounds__(THREADS) void k_distill_resident(DistillArgs a) {
             held[j] = i < pieces_next ? load_piece_once(zn + j * THREADS * kN + at) : nothing<T>();
         }
         last = rest < a.vocab && next < a.rows ? load1(zn + rest) : kNegInf;
+        if (next < a.rows) fetch_logits(zn, entries_next);
         __syncthreads();
+        // entries.q is q times t_sum
+        if (r.has_teacher) d.g_tau /= t_sum;
         if (!zeros) correct_entries<T, POWER, false>(a, r, d, entries, dz);
         __syncthreads();
     }
@@ -593,6 +653,8 @@ int sums_power(const DistillArgs &a) {
 int gradient_power(const DistillArgs &a) {
     return a.distill_weight != 0.0f && a.label_weight != 0.0f && a.labels ? sums_power(a) : 0;
 }
+
+constexpr int kMostHeld = 19;  // pieces a thread, of 1,024: what 128 registers hold beside the work on them
 
 template <typename T, int THREADS, int NV>
 void launch_resident(const DistillArgs &a, int per_cu, hipStream_t s) {
@@ -617,7 +679,7 @@ int64_t pieces_of(const DistillArgs &a, bool bf16) { return a.vocab / (bf16 ? 8 
 // Whether rows stay in registers: a gradient is wanted, a row fits a compute
 // unit's, and there are rows enough to give most units one.
 bool resident(const DistillArgs &a, bool bf16) {
-    return a.dlogits && pieces_of(a, bf16) <= 20 * 1024 && a.rows >= 192;
+    return a.dlogits && pieces_of(a, bf16) <= kMostHeld * 1024 && a.rows >= 192;
 }
 
 template <typename T>
@@ -629,7 +691,7 @@ void launch_resident_any(const DistillArgs &a, hipStream_t s) {
     if (n <= 8 * 1024) return launch_resident<T, 1024, 8>(a, 2, s);
     if (n <= 12 * 1024) return launch_resident<T, 1024, 12>(a, 1, s);
     if (n <= 16 * 1024) return launch_resident<T, 1024, 16>(a, 1, s);
-    return launch_resident<T, 1024, 20>(a, 1, s);
+    return launch_resident<T, 1024, kMostHeld>(a, 1, s);
 }
 
 // Parts of a row so that the grid fills the compute units several times, none
@@ -673,7 +735,7 @@ hipError_t launch_forward(const DistillArgs &a, hipStream_t s) {
     if (a.dlogits)
         launch_gradient<T, false>(a, s);
     else
-        hipLaunchKernelGGL(k_distill_loss, dim3((uint32_t)a.rows), dim3(64), 0, s, a);
+        hipLaunchKernelGGL((k_distill_loss<T>), dim3((uint32_t)a.rows), dim3(64), 0, s, a);
     return hipGetLastError();
 }
 
