@@ -22,11 +22,11 @@
  *    have strides of 0 (a broadcast); an output may not overlap itself.
  *  - An output may overlap an input or another output only where a call says
  *    so; other overlaps are refused.
- *  - Every call is asynchronous on `stream`.  The two calls that use the
- *    context's workspace (sdp_qk_norm_rope_backward, and the distillation
- *    loss where a row is split over blocks) order themselves after the
- *    context's last such call, whatever its stream; a workspace that has to
- *    grow waits for the device.
+ *  - Every call is asynchronous on `stream`.  Calls that use the context's
+ *    workspace (sdp_qk_norm_rope_backward with weight gradients, the
+ *    distillation loss where a row is split over blocks, grouped products of
+ *    few tiles) order themselves after the context's last such call, whatever
+ *    its stream; a workspace that has to grow waits for the device.
  *  - Sums, norms, softmax statistics and products are held in FP32 and an
  *    output is rounded once, to nearest even.  No atomics: the same inputs
  *    give the same bits.
@@ -55,7 +55,7 @@ extern "C" {
 #define SDP_QK_MAX_HEADS 16384
 #define SDP_DISTILL_MAX_K 1024
 #define SDP_DISTILL_MAX_ROWS 4000000
-#define SDP_GROUPED_MAX_GROUPS 4096
+#define SDP_GROUPED_MAX_GROUPS 2048
 
 /* ---- norms of queries and keys with the position rotation ----------------- */
 

@@ -124,96 +124,6 @@ __device__ __forceinline__ void panel_order(int64_t id, int64_t rows, int column
     *column = first + (int)(in_panel - *row * width);
 }
 
-// ---- any size, stride and alignment ----------------------------------------
-
-// A 64 x 64 tile of C, four waves of 32 x 32, 32 of the contraction at a time
-// through LDS, loaded element by element.
-constexpr int kAnyTile = 64, kAnyDepth = 32, kAnyPitch = kAnyDepth + 8;
-
-// 64 x 32 elements (i, c) of base[i * si + c * sc] into LDS, zero outside.
-__device__ void load_any(const uint16_t *base, int64_t si, int64_t sc, int64_t n_i, int64_t n_c,
-                         uint16_t (*lds)[kAnyPitch]) {
-    for (int k = threadIdx.x; k < kAnyTile * kAnyDepth; k += 256) {
-        // neighbouring threads along the contiguous dimension
-        const int i = sc == 1 ? k / kAnyDepth : k % kAnyTile, c = sc == 1 ? k % kAnyDepth : k / kAnyTile;
-        lds[i][c] = i < n_i && c < n_c ? base[i * si + c * sc] : (uint16_t)0;
-    }
-}
-
-template <Mode MODE>
-__global__ __launch_bounds__(256) void k_grouped_any(GroupedArgs a) {
-    __shared__ uint16_t la[kAnyTile][kAnyPitch], lb[kAnyTile][kAnyPitch];
-    int64_t m0, m1, n0, n1, depth;
-    const uint16_t *A = nullptr, *B = nullptr;
-    int64_t sai, sac, sbi, sbc;
-    char *C;
-    int64_t c_stride;
-    bool f32 = a.out_f32 != 0;
-    bool empty = false;
-    const int64_t n_in = a.n_in, n_out = a.n_out;
-    if (MODE == kDw) {
-        const int64_t tm = (n_out + kAnyTile - 1) / kAnyTile, tn = (n_in + kAnyTile - 1) / kAnyTile;
-        const int64_t id = blockIdx.x;
-        const int e = (int)(id / (tm * tn));
-        m0 = (id / tn) % tm * kAnyTile, m1 = n_out;
-        n0 = id % tn * kAnyTile, n1 = n_in;
-        int64_t t0, t1;
-        group_rows(a, e, &t0, &t1);
-        depth = t1 - t0;
-        A = a.dy + t0 * a.y_stride + m0, sai = 1, sac = a.y_stride;
-        B = a.x + t0 * a.x_stride + n0, sbi = 1, sbc = a.x_stride;
-        c_stride = n_in;
-        C = (char *)a.dw + (f32 ? 4 : 2) * ((int64_t)e * n_out * n_in);
-    } else {
-        const int64_t cols = MODE == kForward ? n_out : n_in;
-        const int64_t tn = (cols + kAnyTile - 1) / kAnyTile;
-        const RowTile t = find_row_tile<kAnyTile>(a, (int64_t)blockIdx.x / tn);
-        if (t.group < 0) return;
-        empty = t.group == a.groups;
-        const uint16_t *w = a.w + (empty ? 0 : (int64_t)t.group * n_out * n_in);
-        m0 = t.first, m1 = t.end;
-        n0 = (int64_t)blockIdx.x % tn * kAnyTile, n1 = cols;
-        depth = empty ? 0 : MODE == kForward ? n_in : n_out;
-        if (MODE == kForward) {
-            A = a.x + m0 * a.x_stride, sai = a.x_stride, sac = 1;
-            B = w + n0 * n_in, sbi = n_in, sbc = 1;
-            C = (char *)a.y, c_stride = a.y_stride;
-        } else {
-            A = a.dy + m0 * a.y_stride, sai = a.y_stride, sac = 1;
-            B = w + n0, sbi = 1, sbc = n_in;
-            C = (char *)a.dx, c_stride = a.dx_stride;
-            f32 = false;
-        }
-    }
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int wm = (wave >> 1) * 32, wn = (wave & 1) * 32, sub = lane & 15, quad = lane >> 4;
-    f32x4 acc[2][2] = {};
-    for (int64_t c0 = 0; c0 < depth; c0 += kAnyDepth) {
-        load_any(A + c0 * sac, sai, sac, m1 - m0, depth - c0, la);
-        load_any(B + c0 * sbc, sbi, sbc, n1 - n0, depth - c0, lb);
-        __syncthreads();
-        bf16x8 fa[2], fb[2];
-        for (int i = 0; i < 2; ++i) {
-            fa[i] = *(const bf16x8 *)&la[wm + 16 * i + sub][8 * quad];
-            fb[i] = *(const bf16x8 *)&lb[wn + 16 * i + sub][8 * quad];
-        }
-        for (int i = 0; i < 2; ++i)
-            for (int j = 0; j < 2; ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
-        __syncthreads();
-    }
-    for (int i = 0; i < 2; ++i)
-        for (int j = 0; j < 2; ++j)
-            for (int r = 0; r < 4; ++r) {
-                const int64_t m = m0 + wm + 16 * i + 4 * quad + r, n = n0 + wn + 16 * j + sub;
-                if (m >= m1 || n >= n1) continue;
-                if (f32)
-                    ((float *)C)[m * c_stride + n] = acc[i][j][r];
-                else
-                    store1((uint16_t *)C + m * c_stride + n, acc[i][j][r]);
-            }
-}
-
 // ---- rows of 16-byte pieces ---------------------------------------------------
 
 // Where every row starts at a 16-byte boundary and holds whole pieces of 8
@@ -238,7 +148,7 @@ constexpr uint32_t kRange = 0x7ffffff0u;  // bytes that a load's offset may reac
 
 typedef __attribute__((address_space(3))) void *LdsPtr;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
-typedef __attribute__((ext_vector_type(8))) short s16x8;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
 // The wave of this thread in its block, in a scalar register.
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
@@ -248,6 +158,14 @@ template <int T>
 __device__ __forceinline__ int turn(int d) {
     const int f = (d & 3) | ((d >> 3) & 1) << 2;
     return T >= 128 ? f : f & (T / 16 - 1);
+}
+
+// The lane, worked out where it is used: what depends on it is not to be kept in
+// registers through the steps.
+__device__ __forceinline__ int lane_anew() {
+    int l = threadIdx.x & 63;
+    asm volatile("" : "+v"(l));
+    return l;
 }
 
 // One operand: T elements of its outer dimension (rows of C, or columns) by
@@ -262,9 +180,9 @@ struct Operand {
     uint32_t off[kEach];   // bytes from it of this lane's piece of each load
     int64_t step;          // bytes to the step after
 
-    // outer: how many outer elements exist from the first on (at least 1)
+    // outer: how many outer elements exist from the first on; the others come as 0
     __device__ __forceinline__ void init(const uint16_t *first, int64_t stride, int64_t outer) {
-        const int lane = threadIdx.x & 63, wave = wave_id();
+        const int lane = lane_anew(), wave = wave_id();
         base = (const char *)first;
         step = BY_DEPTH ? kDepth * stride * 2 : kDepth * 2;
 #pragma unroll
@@ -272,14 +190,12 @@ struct Operand {
             const int idx = j * WAVES + wave;
             if (BY_DEPTH) {
                 const int d = (idx * 64 + lane) / kPieces, place = lane % kPieces;
-                int piece = ((place >> 1) ^ turn<T>(d)) * 2 + (place & 1);
-                // past the last element: any piece that exists, its results are not stored
-                if (piece * 8 >= outer) piece = (int)(outer - 1) / 8;
-                off[j] = (uint32_t)d * (uint32_t)(stride * 2) + piece * 16;
+                const int piece = ((place >> 1) ^ turn<T>(d)) * 2 + (place & 1);
+                off[j] = piece * 8 < outer ? (uint32_t)d * (uint32_t)(stride * 2) + piece * 16 : kRange;
             } else {
                 const int r = idx * 16 + lane / 4;
                 const int piece = (lane & 3) ^ (lane >> 3 & 3);
-                off[j] = (uint32_t)(r < outer ? r : (int)outer - 1) * (uint32_t)(stride * 2) + piece * 16;
+                off[j] = r < outer ? (uint32_t)r * (uint32_t)(stride * 2) + piece * 16 : kRange;
             }
         }
     }
@@ -360,6 +276,84 @@ __device__ __forceinline__ void wait_and_meet() {
     asm volatile("" ::: "memory");
 }
 
+// A block's tile of C and its operands.  With splits, blockIdx.y is a part of the
+// contraction, whose product goes to the partial sums.
+struct Place {
+    int64_t m0, m1, n0, n1;  // of C
+    int32_t depth;
+    const uint16_t *A, *B;   // elements (m0, 0) and (n0, 0)
+    int64_t sa, sb;          // by row: from row to row; by depth: from depth to depth
+    char *C;
+    int64_t c_stride;
+    bool f32, none;
+};
+
+template <Mode MODE, int BM, int BN>
+__device__ __forceinline__ Place place_of(const GroupedArgs &a) {
+    Place p;
+    p.none = false;
+    p.f32 = MODE != kDx && a.out_f32 != 0;
+    const int64_t n_in = a.n_in, n_out = a.n_out;
+    int64_t a_depth, b_depth, c_group = 0, c_all;  // elements from depth to depth; of C before this group, and in all
+    if constexpr (MODE == kDw) {
+        const int tm = (int)((n_out + BM - 1) / BM), tn = (int)((n_in + BN - 1) / BN);
+        const int64_t id = xcd_order(blockIdx.x, gridDim.x);
+        const int e = (int)(id / (tm * tn)), in_group = (int)(id - (int64_t)e * (tm * tn));
+        int64_t row;
+        int column;
+        panel_order(in_group, tm, tn, &row, &column);
+        p.m0 = row * BM, p.m1 = n_out;
+        p.n0 = (int64_t)column * BN, p.n1 = n_in;
+        int64_t t0, t1;
+        group_rows(a, e, &t0, &t1);
+        p.depth = (int)(t1 - t0);
+        p.A = a.dy + t0 * a.y_stride + p.m0, p.sa = a_depth = a.y_stride;
+        p.B = a.x + t0 * a.x_stride + p.n0, p.sb = b_depth = a.x_stride;
+        c_group = (int64_t)e * n_out * n_in, c_all = a.groups * n_out * n_in;
+        p.C = (char *)a.dw, p.c_stride = n_in;
+    } else {
+        const int64_t cols = MODE == kForward ? n_out : n_in;
+        const int tn = (int)((cols + BN - 1) / BN);
+        const int64_t tm = find_row_tile<BM>(a, -1).tiles;
+        if (blockIdx.x >= tm * tn) {
+            p.none = true;
+            return p;
+        }
+        int64_t row;
+        int column;
+        panel_order(xcd_order(blockIdx.x, tm * tn), tm, tn, &row, &column);
+        const RowTile t = find_row_tile<BM>(a, row);
+        const bool empty = t.group == a.groups;
+        const uint16_t *w = a.w + (empty ? 0 : (int64_t)t.group * n_out * n_in);
+        p.m0 = t.first, p.m1 = t.end;
+        p.n0 = (int64_t)column * BN, p.n1 = cols;
+        p.depth = empty ? 0 : MODE == kForward ? a.n_in : a.n_out;
+        a_depth = 1;
+        if constexpr (MODE == kForward) {
+            p.A = a.x + p.m0 * a.x_stride, p.sa = a.x_stride;
+            p.B = w + p.n0 * n_in, p.sb = n_in, b_depth = 1;
+            p.C = (char *)a.y, p.c_stride = a.y_stride;
+        } else {
+            p.A = a.dy + p.m0 * a.y_stride, p.sa = a.y_stride;
+            p.B = w + p.n0, p.sb = b_depth = n_in;
+            p.C = (char *)a.dx, p.c_stride = a.dx_stride;
+        }
+        c_all = a.rows * cols;
+    }
+    if (a.splits > 1) {
+        const int steps = (p.depth + kDepth - 1) / kDepth, each = (steps + a.splits - 1) / a.splits;
+        const int from = (int)blockIdx.y * each * kDepth;
+        p.depth = from < p.depth ? min(p.depth - from, each * kDepth) : 0;
+        p.A += p.depth ? from * a_depth : 0;
+        p.B += p.depth ? from * b_depth : 0;
+        p.C = (char *)(a.partials + blockIdx.y * c_all);
+        p.c_stride = p.n1;
+        p.f32 = true;
+    }
+    p.C += (p.f32 ? 4 : 2) * c_group;
+    return p;
+}
+
 template <Mode MODE, int BM, int BN, int WM, int WN, int NB>
 __global__ __launch_bounds__(64 * WM * WN) void k_grouped(GroupedArgs a) {
     constexpr int kWaves = WM * WN, MT = BM / WM / 16, NT = BN / WN / 16;
@@ -372,67 +366,24 @@ __global__ __launch_bounds__(64 * WM * WN) void k_grouped(GroupedArgs a) {
     __shared__ __attribute__((aligned(1024))) char lds0[kBuffer], lds1[kBuffer], lds2[kBuffer];
     __shared__ __attribute__((aligned(1024))) char lds3[kBuffer], lds4[kBuffer], lds5[kBuffer];
 
-    int64_t m0, m1, n0, n1, depth, c_stride;
-    const uint16_t *A, *B;
-    int64_t sa, sb;
-    char *C;
-    bool f32 = a.out_f32 != 0;
-    const int64_t n_in = a.n_in, n_out = a.n_out;
-    if constexpr (MODE == kDw) {
-        const int tm = (int)((n_out + BM - 1) / BM), tn = (int)((n_in + BN - 1) / BN);
-        const int64_t id = xcd_order(blockIdx.x, gridDim.x);
-        const int e = (int)(id / (tm * tn)), in_group = (int)(id - (int64_t)e * (tm * tn));
-        int64_t row;
-        int column;
-        panel_order(in_group, tm, tn, &row, &column);
-        m0 = row * BM, m1 = n_out;
-        n0 = (int64_t)column * BN, n1 = n_in;
-        int64_t t0, t1;
-        group_rows(a, e, &t0, &t1);
-        depth = t1 - t0;
-        A = a.dy + t0 * a.y_stride + m0, sa = a.y_stride;
-        B = a.x + t0 * a.x_stride + n0, sb = a.x_stride;
-        C = (char *)a.dw + (f32 ? 4 : 2) * ((int64_t)e * n_out * n_in), c_stride = n_in;
-    } else {
-        const int64_t cols = MODE == kForward ? n_out : n_in;
-        const int tn = (int)((cols + BN - 1) / BN);
-        const int64_t tm = find_row_tile<BM>(a, -1).tiles;
-        if (blockIdx.x >= tm * tn) return;
-        int64_t row;
-        int column;
-        panel_order(xcd_order(blockIdx.x, tm * tn), tm, tn, &row, &column);
-        const RowTile t = find_row_tile<BM>(a, row);
-        const bool empty = t.group == a.groups;
-        const uint16_t *w = a.w + (empty ? 0 : (int64_t)t.group * n_out * n_in);
-        m0 = t.first, m1 = t.end;
-        n0 = (int64_t)column * BN, n1 = cols;
-        depth = empty ? 0 : MODE == kForward ? n_in : n_out;
-        if constexpr (MODE == kForward) {
-            A = a.x + m0 * a.x_stride, sa = a.x_stride;
-            B = w + n0 * n_in, sb = n_in;
-            C = (char *)a.y, c_stride = a.y_stride;
-        } else {
-            A = a.dy + m0 * a.y_stride, sa = a.y_stride;
-            B = w + n0, sb = n_in;
-            C = (char *)a.dx, c_stride = a.dx_stride;
-            f32 = false;
-        }
-    }
+    const Place at = place_of<MODE, BM, BN>(a);
+    if (at.none) return;
+    const int64_t m0 = at.m0, m1 = at.m1, n0 = at.n0, n1 = at.n1;
 
     // the waves' 16-row fragments alternate, so that a tile with few rows is
     // shared by all of them; their columns lie together
     const int wave = wave_id(), lane = threadIdx.x & 63;
     const int wm = wave / WN * 16, wn = wave % WN * (BN / WN);
     f32x4 acc[MT][NT] = {};
-    const int steps = (int)((depth + kDepth - 1) / kDepth);
+    const int steps = (at.depth + kDepth - 1) / kDepth;
     // the whole contraction, over the first MU of a wave's row fragments
     auto contract = [&](auto used) __attribute__((always_inline)) {
         constexpr int MU = decltype(used)::value;
         constexpr int kLoads = OpA::template loads<MU * WM * 16>() + OpB::template loads<BN>();
         OpA oa;
         OpB ob;
-        oa.init(A, sa, m1 - m0);
-        ob.init(B, sb, n1 - n0);
+        oa.init(at.A, at.sa, m1 - m0);
+        ob.init(at.B, at.sb, n1 - n0);
         Reader<BM, kADepth, WM> ra;
         Reader<BN, kBDepth, 1> rb;
         ra.init(wm);
@@ -444,7 +395,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_grouped(GroupedArgs a) {
 #pragma unroll
             for (int i = 0; i < MU; ++i) fa[f][i] = ra.read(lds, i);
         };
-        int left = (int)depth;  // of the contraction, to load
+        int left = at.depth;  // of the contraction, to load
         auto load = [&](char *lds) __attribute__((always_inline)) {
             oa.template load<MU * WM * 16>(lds, left);
             ob.template load<BN>(lds + OpA::kBytes, left);
@@ -506,16 +457,407 @@ __global__ __launch_bounds__(64 * WM * WN) void k_grouped(GroupedArgs a) {
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
                 const int64_t n = n0 + wn + 16 * j + 4 * (lane >> 4);
-                if (n < n1) put(m * c_stride + n, acc[i][j]);
+                if (n < n1) put(m * at.c_stride + n, acc[i][j]);
             }
         }
     };
-    if (f32)
-        store([&](int64_t at, f32x4 v) { *(f32x4 *)((float *)C + at) = v; });
+    if (at.f32)
+        store([&](int64_t i, f32x4 v) { *(f32x4 *)((float *)at.C + i) = v; });
     else
-        store([&](int64_t at, f32x4 v) {
-            *(uint2 *)((uint16_t *)C + at) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+        store([&](int64_t i, f32x4 v) {
+            *(uint2 *)((uint16_t *)at.C + i) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
         });
+}
+
+// ---- any size, stride and alignment ---------------------------------------------
+
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+
+// An operand whose rows start and end anywhere: the same tile in LDS, its 16-byte
+// pieces loaded into registers (element by element at the edges) and written there.
+template <int T, bool BY_DEPTH, int THREADS>
+struct Loose {
+    static constexpr int kEach = T * kDepth * 2 / 16 / THREADS;
+    static constexpr int kBytes = T * kDepth * 2;
+    static constexpr int kPieces = T / 8;
+    const uint16_t *first;
+    int64_t stride;
+    int32_t outer;
+    u32x4 held[kEach];
+
+    __device__ __forceinline__ void init(const uint16_t *first_, int64_t stride_, int64_t outer_) {
+        first = first_, stride = stride_, outer = outer_ < T ? (int32_t)outer_ : T;
+    }
+    // Depths from k on, `left` of them being there.
+    __device__ __forceinline__ void load(int64_t k, int left) {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            const int q = j * THREADS + threadIdx.x;
+            const int r = BY_DEPTH ? q / kPieces : q / 4;
+            const int place = BY_DEPTH ? q % kPieces : q & 3;
+            const int piece = BY_DEPTH ? ((place >> 1) ^ turn<T>(r)) * 2 + (place & 1) : place ^ (r >> 1 & 3);
+            const bool there = BY_DEPTH ? r < left : r < outer;
+            const int n = (BY_DEPTH ? outer : left) - piece * 8;  // elements from the piece's first on
+            const uint16_t *p = first + (BY_DEPTH ? (k + r) * stride : r * stride + k) + piece * 8;
+            u32x4 v = {0, 0, 0, 0};
+            if (there && n >= 8) {
+                v = *(const u32x4_any *)p;
+            } else if (there && n > 0) {
+#pragma unroll
+                for (int e = 0; e < 7; ++e)
+                    if (e < n) v[e / 2] |= (uint32_t)p[e] << (e % 2 * 16);
+            }
+            held[j] = v;
+        }
+    }
+    __device__ __forceinline__ void write(char *lds) const {
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) *(u32x4 *)(lds + (j * THREADS + threadIdx.x) * 16) = held[j];
+    }
+};
+
+// T x T tiles, four waves; two buffers, and the next step's pieces in registers
+// while this one's products run.
+template <Mode MODE, int T>
+__global__ __launch_bounds__(256) void k_grouped_loose(GroupedArgs a) {
+    constexpr int kTiles = T / 2 / 16;  // 16 x 16 tiles of a wave, each way
+    constexpr bool kADepth = MODE == kDw, kBDepth = MODE != kForward;
+    using OpA = Loose<T, kADepth, 256>;
+    using OpB = Loose<T, kBDepth, 256>;
+    __shared__ __attribute__((aligned(1024))) char lds_a[2][OpA::kBytes], lds_b[2][OpB::kBytes];
+    const Place at = place_of<MODE, T, T>(a);
+    if (at.none) return;
+    const int wave = wave_id(), lane = threadIdx.x & 63, wm = wave / 2 * (T / 2), wn = wave % 2 * (T / 2);
+    OpA oa;
+    OpB ob;
+    oa.init(at.A, at.sa, at.m1 - at.m0);
+    ob.init(at.B, at.sb, at.n1 - at.n0);
+    Reader<T, kADepth, 1> ra;
+    Reader<T, kBDepth, 1> rb;
+    ra.init(wm);
+    rb.init(wn);
+    f32x4 acc[kTiles][kTiles] = {};
+    const int steps = (at.depth + kDepth - 1) / kDepth;
+    if (steps > 0) {
+        oa.load(0, at.depth);
+        ob.load(0, at.depth);
+    }
+    for (int k = 0; k < steps; ++k) {
+        char *la = lds_a[k & 1], *lb = lds_b[k & 1];
+        oa.write(la);
+        ob.write(lb);
+        __syncthreads();
+        if (k + 1 < steps) {
+            oa.load((int64_t)(k + 1) * kDepth, at.depth - (k + 1) * kDepth);
+            ob.load((int64_t)(k + 1) * kDepth, at.depth - (k + 1) * kDepth);
+        }
+        bf16x8 fa[kTiles], fb[kTiles];
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i) fa[i] = ra.read(la, i), fb[i] = rb.read(lb, i);
+#pragma unroll
+        for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+            for (int j = 0; j < kTiles; ++j)
+                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < kTiles; ++i) {
+        const int64_t m = at.m0 + wm + 16 * i + (lane & 15);
+        if (m >= at.m1) continue;
+#pragma unroll
+        for (int j = 0; j < kTiles; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int64_t n = at.n0 + wn + 16 * j + 4 * (lane >> 4) + r;
+                if (n >= at.n1) continue;
+                if (at.f32)
+                    ((float *)at.C)[m * at.c_stride + n] = acc[i][j][r];
+                else
+                    store1((uint16_t *)at.C + m * at.c_stride + n, acc[i][j][r]);
+            }
+    }
+}
+
+// The partial sums of `elems` results in rows of `cols`, added in order and rounded.
+__global__ __launch_bounds__(256) void k_grouped_join(const float *partials, int splits, int64_t elems, int32_t cols,
+                                                      char *out, int64_t stride, int f32) {
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < elems; i += (int64_t)gridDim.x * 256) {
+        float v = 0.0f;
+        for (int k = 0; k < splits; ++k) v += partials[k * elems + i];
+        const int64_t row = i / cols, to = row * stride + (i - row * cols);
+        if (f32)
+            ((float *)out)[to] = v;
+        else
+            store1((uint16_t *)out + to, v);
+    }
+}
+
+// ---- many tiles --------------------------------------------------------------------
+
+// 256 x 256 tiles, one block to a compute unit, each block walking its share of the
+// tiles as one stream of steps: the last steps of a tile load the first ones of
+// the next, and a tile's results are stored while the next one's products run.
+// (Tile by tile, with a launch of one block each, the fixed cost of a tile was 15 us,
+// next to 28 us for a contraction of 1,024.)
+constexpr int kStreamBlocks = 256, kStreamTile = 256, kStreamWm = 2, kStreamWn = 4, kStreamNb = 4;
+constexpr int kSortedGroups = 256;  // dw: up to so many groups are taken largest first
+
+template <Mode MODE>
+__global__ __launch_bounds__(512) void k_grouped_stream(GroupedArgs a) {
+    constexpr int BM = kStreamTile, BN = kStreamTile, WM = kStreamWm, WN = kStreamWn, NB = kStreamNb;
+    constexpr int kWaves = WM * WN, MT = BM / WM / 16, NT = BN / WN / 16;
+    constexpr bool kADepth = MODE == kDw, kBDepth = MODE != kForward;
+    using OpA = Operand<BM, kADepth, kWaves>;
+    using OpB = Operand<BN, kBDepth, kWaves>;
+    constexpr int kBuffer = OpA::kBytes + OpB::kBytes;
+    constexpr int kLoads = OpA::template loads<BM>() + OpB::template loads<BN>(), kStores = MT * NT;
+    __shared__ __attribute__((aligned(1024))) char lds0[kBuffer], lds1[kBuffer], lds2[kBuffer], lds3[kBuffer];
+    // of each group (the last: the rows of none): its end, and the row tiles before it
+    __shared__ int32_t ends[SDP_GROUPED_MAX_GROUPS + 1], tiles_before[SDP_GROUPED_MAX_GROUPS + 2];
+    __shared__ int16_t by_size[kSortedGroups];
+
+    const int lane = threadIdx.x & 63, wave = wave_id();
+    if (wave == 0) {
+        int64_t run = 0;
+        int32_t tiles = 0;
+        for (int base = 0; base <= a.groups; base += 64) {
+            const int e = base + lane;
+            const int64_t end = group_end(a, e, run);
+            int64_t start = shfl_up64(end, 1);
+            if (lane == 0) start = run;
+            const int32_t mine = e <= a.groups ? (int32_t)((end - start + BM - 1) / BM) : 0;
+            int32_t upto = mine;
+            for (int d = 1; d < 64; d <<= 1) {
+                const int32_t before = __shfl_up(upto, d);
+                if (lane >= d) upto += before;
+            }
+            if (e <= a.groups) ends[e] = (int32_t)end, tiles_before[e] = tiles + upto - mine;
+            run = shfl64(end, 63);
+            tiles += __shfl(upto, 63);
+        }
+        if (lane == 0) tiles_before[a.groups + 1] = tiles;
+    }
+    __syncthreads();
+    const bool sorted = MODE == kDw && a.groups <= kSortedGroups;
+    if (sorted) {
+        for (int e = threadIdx.x; e < a.groups; e += 512) {
+            const int32_t size = ends[e] - (e ? ends[e - 1] : 0);
+            int rank = 0;
+            for (int f = 0; f < a.groups; ++f) {
+                const int32_t other = ends[f] - (f ? ends[f - 1] : 0);
+                rank += other > size || (other == size && f < e);
+            }
+            by_size[rank] = (int16_t)e;
+        }
+        __syncthreads();
+    }
+
+    const int64_t n_in = a.n_in, n_out = a.n_out;
+    const int64_t cols = MODE == kForward ? n_out : n_in;
+    const int tn = (int)((cols + BN - 1) / BN);
+    const int64_t tm = MODE == kDw ? (n_out + BM - 1) / BM
+                                   : __builtin_amdgcn_readfirstlane(tiles_before[a.groups + 1]);
+    const int64_t total = MODE == kDw ? tm * tn * a.groups : tm * tn;
+
+    // The block's tile of round r.  A round's 256 tiles are neighbours, 32 of them
+    // to an XCD; for dw, where the groups' sizes make tiles cost more or less and they
+    // come sorted, every other round goes the other way round.
+    auto tile_id = [&](int r) {
+        const int place = (int)(blockIdx.x & 7) * (kStreamBlocks / 8) + (int)(blockIdx.x >> 3);
+        return (int64_t)r * kStreamBlocks + (sorted && (r & 1) ? kStreamBlocks - 1 - place : place);
+    };
+    struct Tile {
+        const uint16_t *A, *B;
+        char *C;
+        int32_t rows, columns, depth;  // that exist
+    };
+    const int64_t sa = MODE == kForward ? a.x_stride : a.y_stride, sb = MODE == kDw ? a.x_stride : n_in;
+    const int64_t c_stride = MODE == kForward ? a.y_stride : MODE == kDx ? a.dx_stride : n_in;
+    const bool f32 = MODE != kDx && a.out_f32;
+    const int c_size = f32 ? 4 : 2;
+    auto tile = [&](int64_t id) {
+        Tile t;
+        int64_t row;
+        int column;
+        if constexpr (MODE == kDw) {
+            const int64_t g = id / (tm * tn);
+            panel_order(id - g * (tm * tn), tm, tn, &row, &column);
+            const int e = sorted ? __builtin_amdgcn_readfirstlane(by_size[g]) : (int)g;
+            const int t0 = e ? __builtin_amdgcn_readfirstlane(ends[e - 1]) : 0;
+            t.depth = __builtin_amdgcn_readfirstlane(ends[e]) - t0;
+            t.A = a.dy + t0 * a.y_stride + row * BM;
+            t.B = a.x + t0 * a.x_stride + (int64_t)column * BN;
+            t.rows = (int)(n_out - row * BM);
+            t.C = (char *)a.dw + c_size * ((e * n_out + row * BM) * n_in + (int64_t)column * BN);
+        } else {
+            panel_order(id, tm, tn, &row, &column);
+            // the last group with at most `row` tiles before it, 64 at a time
+            const int n = a.groups + 1, step = (n + 63) / 64;
+            const int far = lane * step;
+            const int hits = __popcll(__ballot(far < n && tiles_before[far < n ? far : 0] <= row));
+            const int base = (hits - 1) * step, near = base + lane;
+            const int more = __popcll(__ballot(lane < step && near < n && tiles_before[near < n ? near : 0] <= row));
+            const int e = base + more - 1;
+            const int start = e ? __builtin_amdgcn_readfirstlane(ends[e - 1]) : 0;
+            const int64_t m0 = start + (row - __builtin_amdgcn_readfirstlane(tiles_before[e])) * BM;
+            const bool empty = e == a.groups;
+            const uint16_t *w = a.w + (empty ? 0 : e * n_out * n_in);
+            t.rows = __builtin_amdgcn_readfirstlane(ends[e]) - (int)m0;
+            t.depth = empty ? 0 : MODE == kForward ? a.n_in : a.n_out;
+            if constexpr (MODE == kForward) {
+                t.A = a.x + m0 * a.x_stride;
+                t.B = w + (int64_t)column * BN * n_in;
+                t.C = (char *)a.y + c_size * (m0 * a.y_stride + (int64_t)column * BN);
+            } else {
+                t.A = a.dy + m0 * a.y_stride;
+                t.B = w + (int64_t)column * BN;
+                t.C = (char *)a.dx + c_size * (m0 * a.dx_stride + (int64_t)column * BN);
+            }
+        }
+        t.columns = (int)(cols - (int64_t)column * BN);
+        return t;
+    };
+
+    int round = 0;
+    if (tile_id(0) >= total) return;
+    Tile cur = tile(tile_id(0));
+    OpA oa;
+    OpB ob;
+    int left = cur.depth;  // of the contraction that is being loaded
+    oa.init(cur.A, sa, cur.rows);
+    ob.init(cur.B, sb, cur.columns);
+    auto load = [&](char *lds) __attribute__((always_inline)) {
+        oa.template load<BM>(lds, left);
+        ob.template load<BN>(lds + OpA::kBytes, left);
+        left = left > kDepth ? left - kDepth : 0;
+    };
+    const int wm = wave / WN * 16, wn = wave % WN * (BN / WN);
+    Reader<BM, kADepth, WM> ra;
+    Reader<BN, kBDepth, 1> rb;
+    ra.init(wm);
+    rb.init(wn);
+    f32x4 acc[MT][NT] = {};
+    bf16x8 fa[MT], fb[2][NT];
+    bool stored = false;  // the stores of a tile lie between the loads in flight
+
+    int used = MT;  // row fragments that have rows: MT, or a half or a quarter of them
+
+    // Step u of four.  In the first three after a tile's stores those may still be
+    // in flight, in front of none of the loads that are waited for.
+    auto step = [&](int u, char *lds, const char *next) __attribute__((always_inline)) {
+        // (the scalars are hidden from the compiler, which would otherwise make a loop
+        // of its own for each value, and run out of registers between them)
+        int mu = used, after = stored;
+        asm volatile("" : "+s"(mu), "+s"(after));
+        if (u < 3 && after)
+            wait_and_meet<(NB - 2) * kLoads + kStores>();
+        else
+            wait_and_meet<(NB - 2) * kLoads>();
+        load(lds);
+        const int f = u & 1;
+        // A row fragment is read anew for the next step as soon as its products are
+        // under way; the last step reads all of them, for whatever tile comes next.
+        auto rows = [&](int i0, int i1) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                if (i < i0 || i >= i1) continue;
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[f][j], fa[i], acc[i][j], 0, 0, 0);
+                fa[i] = ra.read(next, i);
+                if (i < NT / 2) {
+                    fb[f ^ 1][2 * i] = rb.read(next + OpA::kBytes, 2 * i);
+                    fb[f ^ 1][2 * i + 1] = rb.read(next + OpA::kBytes, 2 * i + 1);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        auto reread = [&](int i0, int i1) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                if (i >= i0 && i < i1) fa[i] = ra.read(next, i);
+        };
+        rows(0, MT / 4);
+        if (mu > MT / 4)
+            rows(MT / 4, MT / 2);
+        else if (u == 3)
+            reread(MT / 4, MT / 2);
+        if (mu > MT / 2)
+            rows(MT / 2, MT);
+        else if (u == 3)
+            reread(MT / 2, MT);
+    };
+
+    load(lds0);
+    load(lds1);
+    load(lds2);
+    load(lds3);
+    wait_and_meet<(NB - 1) * kLoads>();
+#pragma unroll
+    for (int j = 0; j < NT; ++j) fb[0][j] = rb.read(lds0 + OpA::kBytes, j);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) fa[i] = ra.read(lds0, i);
+
+    for (;;) {
+        // whole fours: past the contraction loads bring zeros
+        const int fours = cur.depth > 0 ? (cur.depth + 4 * kDepth - 1) / (4 * kDepth) : 1;
+        const int64_t next_id = tile_id(round + 1);
+        const bool has_next = next_id < total;
+        Tile next = cur;
+        used = cur.rows <= BM / 4 ? MT / 4 : cur.rows <= BM / 2 ? MT / 2 : MT;
+        for (int k = 0; k < fours; ++k) {
+            if (k == fours - 1) {
+                // from here on the loads are the next tile's
+                left = 0;
+                if (has_next) {
+                    next = tile(next_id);
+                    oa.init(next.A, sa, next.rows);
+                    ob.init(next.B, sb, next.columns);
+                    left = next.depth;
+                }
+            }
+            step(0, lds0, lds1);
+            step(1, lds1, lds2);
+            step(2, lds2, lds3);
+            step(3, lds3, lds0);
+            stored = false;
+        }
+        // a lane holds 4 neighbouring columns of row lane % 16 of each 16 x 16 tile;
+        // all kStores are issued, those past the tile's end to an offset out of range
+        const __amdgpu_buffer_rsrc_t c = __builtin_amdgcn_make_buffer_rsrc(cur.C, 0, kRange, 0x00020000);
+        const int l = lane_anew();
+        const int m = wm + (l & 15), n = wn + 4 * (l >> 4);
+        const uint32_t row_bytes = (uint32_t)(c_stride * c_size);
+        auto store = [&](auto put) __attribute__((always_inline)) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                const int mi = m + 16 * WM * i;
+                const uint32_t at = (uint32_t)mi * row_bytes + n * c_size;
+#pragma unroll
+                for (int j = 0; j < NT; ++j)
+                    put(mi < cur.rows && n + 16 * j < cur.columns ? at + 16 * j * c_size : kRange, acc[i][j]);
+            }
+        };
+        if (f32)
+            store([&](uint32_t o, f32x4 v) {
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), c, o, 0, 0);
+            });
+        else
+            store([&](uint32_t o, f32x4 v) {
+                __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack2(v[0], v[1]), pack2(v[2], v[3])}, c, o, 0, 0);
+            });
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0, 0, 0, 0};
+        if (!has_next) break;
+        cur = next;
+        ++round;
+        stored = true;
+    }
+    // no load may land after the block has given its LDS back
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(15 << 8 | 7 << 4);
 }
 
 int64_t ceil_div(int64_t a, int64_t b) { return a / b + (a % b != 0); }
@@ -528,25 +870,12 @@ int64_t row_tiles(const GroupedArgs &a, int64_t bm) {
     return most < a.rows ? most : a.rows;
 }
 
-constexpr int64_t kMaxBlocks = 0xffffffffll / 256;
-
-int64_t blocks_any(const GroupedArgs &a, Mode mode) {
-    if (mode == kDw) return (int64_t)a.groups * ceil_div(a.n_out, kAnyTile) * ceil_div(a.n_in, kAnyTile);
-    return row_tiles(a, kAnyTile) * ceil_div(mode == kForward ? a.n_out : a.n_in, kAnyTile);
-}
-
-template <Mode MODE>
-hipError_t launch_any(const GroupedArgs &a, hipStream_t s) {
-    const int64_t blocks = blocks_any(a, MODE);
-    if (blocks == 0) return hipSuccess;
-    hipLaunchKernelGGL((k_grouped_any<MODE>), dim3((uint32_t)blocks), dim3(256), 0, s, a);
-    return hipGetLastError();
-}
+constexpr int64_t kMaxBlocks = 0xffffffffll / 512;
 
 // Whether the tiled kernels can take the call: whole 16-byte pieces in every
-// row, rows and results at 16-byte boundaries, and a tile's offsets in 32 bits.
+// row, rows and results at 16-byte boundaries, and a tile's offsets in 31 bits.
 bool pieces(const void *p, int64_t stride, int64_t cols) {
-    return (uintptr_t)p % 16 == 0 && stride % 8 == 0 && cols % 8 == 0 && stride < ((int64_t)1 << 22);
+    return (uintptr_t)p % 16 == 0 && stride % 8 == 0 && cols % 8 == 0 && stride < ((int64_t)1 << 21);
 }
 bool tiled(const GroupedArgs &a, Mode mode) {
     const bool w = mode == kDw || pieces(a.w, a.n_in, a.n_in);
@@ -554,43 +883,122 @@ bool tiled(const GroupedArgs &a, Mode mode) {
     const bool dy = mode == kForward || pieces(a.dy, a.y_stride, a.n_out);
     const void *c = mode == kForward ? a.y : mode == kDx ? (const void *)a.dx : a.dw;
     const int64_t cs = mode == kForward ? a.y_stride : mode == kDx ? a.dx_stride : a.n_in;
-    return w && x && dy && (uintptr_t)c % 16 == 0 && cs % 4 == 0 && a.n_in % 8 == 0 && a.n_out % 8 == 0;
+    return w && x && dy && (uintptr_t)c % 16 == 0 && cs % 4 == 0 && cs < ((int64_t)1 << 21) && a.n_in % 8 == 0 &&
+           a.n_out % 8 == 0;
 }
 
-// Row tiles of bm rows that the groups make if each leaves half a tile, and the
-// tiles of a product.
-template <Mode MODE>
-int64_t likely_tiles(const GroupedArgs &a, int64_t bm, int64_t bn) {
-    if (MODE == kDw) return (int64_t)a.groups * ceil_div(a.n_out, bm) * ceil_div(a.n_in, bn);
+int64_t columns_of(const GroupedArgs &a, Mode mode) { return mode == kForward ? a.n_out : a.n_in; }
+int64_t results_of(const GroupedArgs &a, Mode mode) {
+    return mode == kDw ? (int64_t)a.groups * a.n_out * a.n_in : a.rows * columns_of(a, mode);
+}
+
+// Tiles of t x t that a product makes if each group leaves half a row tile; and the
+// most that it can make.
+int64_t likely_tiles(const GroupedArgs &a, Mode mode, int64_t t) {
+    if (mode == kDw) return (int64_t)a.groups * ceil_div(a.n_out, t) * ceil_div(a.n_in, t);
     const int64_t parts = a.groups < a.rows ? a.groups : a.rows;
-    return (ceil_div(a.rows, bm) + parts / 2) * ceil_div(MODE == kForward ? a.n_out : a.n_in, bn);
+    return (ceil_div(a.rows, t) + parts / 2) * ceil_div(columns_of(a, mode), t);
+}
+int64_t most_tiles(const GroupedArgs &a, Mode mode, int64_t t) {
+    return mode == kDw ? likely_tiles(a, mode, t) : row_tiles(a, t) * ceil_div(columns_of(a, mode), t);
 }
 
-template <Mode MODE, int BM, int BN, int WM, int WN, int NB>
-hipError_t launch_tiled(const GroupedArgs &a, hipStream_t s) {
-    const int64_t blocks = MODE == kDw ? likely_tiles<kDw>(a, BM, BN)
-                                       : row_tiles(a, BM) * ceil_div(MODE == kForward ? a.n_out : a.n_in, BN);
-    if (blocks == 0) return hipSuccess;
-    hipLaunchKernelGGL((k_grouped<MODE, BM, BN, WM, WN, NB>), dim3((uint32_t)blocks), dim3(64 * WM * WN), 0, s, a);
+// How a product is done: in one stream of 256 x 256 tiles, in tiles of `tile`, or
+// (loose) in tiles loaded through registers; and in how many parts of the
+// contraction.
+struct Way {
+    bool stream, loose;
+    int tile, splits;
+};
+
+// The largest tile that still occupies the 256 compute units, as it loads the fewest
+// bytes for its products.  From 256 tiles of 256 on and with two groups or more they
+// are walked as a stream, which also evens out groups of different sizes (16,384 rows,
+// 8 groups, 2048 x 2048, dw: 166 us against 199 in blocks of one tile; 65,536 rows,
+// 64 groups, 2048 x 1536: 513 against 591); one group alone fares better in blocks
+// (4096^2 x 8192, dw: 209 us against 249).  Measured with weights from memory:
+// 8,192 rows, 16 groups, 1024 x 1024, 160 tiles of 256: 39 us (128: 44); 4,096 rows,
+// 8 groups, 2048 -> 1536, 120 tiles: 62 us (128: 51, 64: 76); 1,000 rows, 16 groups,
+// 2048 -> 1024, 128 tiles of 128: 32 us (64: 33); 64 rows, one group, 2048 x 2048, 16
+// tiles of 128: 19 us (64: 15).  Where even tiles of 64 are few, parts of the
+// contraction are done by blocks of their own, of 8 steps at least.
+Way way_of(const GroupedArgs &a, Mode mode) {
+    const int64_t t256 = likely_tiles(a, mode, 256), t128 = likely_tiles(a, mode, 128), t64 = likely_tiles(a, mode, 64);
+    Way w{false, !tiled(a, mode), 64, 1};
+    if (!w.loose && a.groups >= 2 && t256 >= (mode == kDw ? 257 : 256)) {
+        w.stream = true;
+        w.tile = 256;
+    } else if (!w.loose && t256 >= 150) {
+        w.tile = 256;
+    } else if (t128 >= 150) {
+        w.tile = 128;
+    } else if (t64 > 0 && t64 < 384) {
+        const int64_t depth = mode == kForward ? a.n_in : mode == kDx ? a.n_out : a.rows / (a.groups ? a.groups : 1);
+        int64_t n = 1024 / t64;
+        n = n < depth / (8 * kDepth) ? n : depth / (8 * kDepth);
+        n = n < 16 ? n : 16;
+        const int64_t bytes = 4 * results_of(a, mode), room = bytes ? ((int64_t)64 << 20) / bytes : 1;
+        n = n < room ? n : room;
+        w.splits = n > 1 ? (int)n : 1;
+    }
+    return w;
+}
+
+template <Mode MODE, int T, int WM, int WN, int NB>
+void launch_tiled(const GroupedArgs &a, hipStream_t s) {
+    const dim3 grid((uint32_t)most_tiles(a, MODE, T), a.splits);
+    hipLaunchKernelGGL((k_grouped<MODE, T, T, WM, WN, NB>), grid, dim3(64 * WM * WN), 0, s, a);
+}
+template <Mode MODE, int T>
+void launch_loose(const GroupedArgs &a, hipStream_t s) {
+    const dim3 grid((uint32_t)most_tiles(a, MODE, T), a.splits);
+    hipLaunchKernelGGL((k_grouped_loose<MODE, T>), grid, dim3(256), 0, s, a);
+}
+
+template <Mode MODE>
+hipError_t launch(const GroupedArgs &args, hipStream_t s) {
+    GroupedArgs a = args;
+    const Way w = way_of(a, MODE);
+    if (most_tiles(a, MODE, w.tile) == 0) return hipSuccess;
+    a.splits = w.splits;
+    if (w.stream)
+        hipLaunchKernelGGL((k_grouped_stream<MODE>), dim3(kStreamBlocks), dim3(512), 0, s, a);
+    else if (w.loose)
+        w.tile == 128 ? launch_loose<MODE, 128>(a, s) : launch_loose<MODE, 64>(a, s);
+    else if (w.tile == 256)
+        launch_tiled<MODE, 256, 2, 4, 4>(a, s);
+    else if (w.tile == 128)
+        launch_tiled<MODE, 128, 2, 2, 4>(a, s);
+    else
+        launch_tiled<MODE, 64, 2, 2, 6>(a, s);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || w.splits == 1) return e;
+    const int64_t elems = results_of(a, MODE), blocks = ceil_div(elems, 256);
+    char *out = (char *)(MODE == kForward ? a.y : MODE == kDx ? (void *)a.dx : a.dw);
+    hipLaunchKernelGGL(k_grouped_join, dim3((uint32_t)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, a.partials,
+                       w.splits, elems, (int32_t)columns_of(a, MODE), out,
+                       MODE == kForward ? a.y_stride : MODE == kDx ? a.dx_stride : (int64_t)a.n_in,
+                       MODE != kDx && a.out_f32);
     return hipGetLastError();
 }
 
-// The largest tile whose tiles still occupy the 256 compute units (a large tile
-// moves fewer operand bytes for its products, but takes a unit to itself; two
-// blocks of the smaller ones share one).
-template <Mode MODE>
-hipError_t launch(const GroupedArgs &a, hipStream_t s) {
-    if (!tiled(a, MODE)) return launch_any<MODE>(a, s);
-    if (likely_tiles<MODE>(a, 256, 256) >= 512) return launch_tiled<MODE, 256, 256, 2, 4, 4>(a, s);
-    if (likely_tiles<MODE>(a, 128, 128) >= 192) return launch_tiled<MODE, 128, 128, 2, 2, 4>(a, s);
-    return launch_tiled<MODE, 64, 128, 2, 2, 6>(a, s);
+bool fits(const GroupedArgs &a, Mode mode) { return most_tiles(a, mode, way_of(a, mode).tile) <= kMaxBlocks; }
+size_t partial_bytes(const GroupedArgs &a, Mode mode) {
+    const Way w = way_of(a, mode);
+    return w.splits > 1 ? (size_t)w.splits * (size_t)results_of(a, mode) * 4 : 0;
 }
 
 }  // namespace
 
 bool grouped_fits(const GroupedArgs &a, bool forward, bool dx, bool dw) {
-    return (!forward || blocks_any(a, kForward) <= kMaxBlocks) && (!dx || blocks_any(a, kDx) <= kMaxBlocks) &&
-           (!dw || blocks_any(a, kDw) <= kMaxBlocks);
+    return (!forward || fits(a, kForward)) && (!dx || fits(a, kDx)) && (!dw || fits(a, kDw));
+}
+
+size_t grouped_workspace(const GroupedArgs &a, bool forward, bool dx, bool dw) {
+    size_t n = forward ? partial_bytes(a, kForward) : 0;
+    if (dx && partial_bytes(a, kDx) > n) n = partial_bytes(a, kDx);
+    if (dw && partial_bytes(a, kDw) > n) n = partial_bytes(a, kDw);
+    return n;
 }
 
 hipError_t launch_grouped_forward(const GroupedArgs &a, hipStream_t s) { return launch<kForward>(a, s); }

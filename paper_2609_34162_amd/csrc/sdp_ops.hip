@@ -259,6 +259,21 @@ int check_grids(const char *call, const sdpops::GroupedArgs &a, bool forward, bo
     return SDP_OK;
 }
 
+// The products of a call, in the workspace where one is split.
+int run_grouped(sdp_ctx *ctx, sdpops::GroupedArgs &a, bool forward, bool dx, bool dw, hipStream_t s) {
+    const size_t bytes = sdpops::grouped_workspace(a, forward, dx, dw);
+    if (bytes > 0) {
+        SDP_TRY(ensure_ops_space(ctx, bytes));
+        a.partials = (float *)ctx->ops_space;
+        SDP_TRY(ops_order(ctx, s));
+    }
+    if (forward) HIP_TRY(sdpops::launch_grouped_forward(a, s));
+    if (dx) HIP_TRY(sdpops::launch_grouped_dx(a, s));
+    if (dw) HIP_TRY(sdpops::launch_grouped_dw(a, s));
+    if (bytes > 0) SDP_TRY(ops_mark(ctx, s));
+    return SDP_OK;
+}
+
 // ---- distillation ----------------------------------------------------------------
 
 int distill_call(sdp_ctx *ctx, const char *call, const sdp_distill_desc *d, float *loss, float *lse,
@@ -399,8 +414,7 @@ int sdp_grouped_matmul(sdp_ctx *ctx, const sdp_grouped_desc *desc, const uint16_
                                dense("ends", desc->ends, desc->groups, type_size(desc->ends_type), false),
                                rows_of("y", y, desc->rows, desc->y_stride, out, type_size(desc->out_type), true)},
                               {}));
-        HIP_TRY(sdpops::launch_grouped_forward(a, (hipStream_t)stream));
-        return SDP_OK;
+        return run_grouped(ctx, a, true, false, false, (hipStream_t)stream);
     });
 }
 
@@ -429,9 +443,7 @@ int sdp_grouped_matmul_backward(sdp_ctx *ctx, const sdp_grouped_desc *desc, cons
             ts.push_back(dense("dw", dw, desc->groups * out * in, type_size(desc->out_type), true));
         }
         SDP_TRY(check_tensors(ctx, call, ts, {}));
-        if (dx) HIP_TRY(sdpops::launch_grouped_dx(a, (hipStream_t)stream));
-        if (dw) HIP_TRY(sdpops::launch_grouped_dw(a, (hipStream_t)stream));
-        return SDP_OK;
+        return run_grouped(ctx, a, false, dx != nullptr, dw != nullptr, (hipStream_t)stream);
     });
 }
 

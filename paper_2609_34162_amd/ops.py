@@ -21,7 +21,7 @@ SDP_QK_MAX_HEAD_DIM = 1024
 SDP_QK_MAX_HEADS = 16384
 SDP_DISTILL_MAX_K = 1024
 SDP_DISTILL_MAX_ROWS = 4000000
-SDP_GROUPED_MAX_GROUPS = 4096
+SDP_GROUPED_MAX_GROUPS = 2048
 
 
 class sdp_heads(ctypes.Structure):

@@ -85,6 +85,51 @@ def test_long_contractions(ctx, n_in, n_out):
     check_all(ctx, [700, 1500, 333], n_in, n_out, out=F32, seed=1)
 
 
+MANY = [0, 1, 63, 64, 65, 0, 127, 128, 129, 256, 257, 300, 0, 5, 17, 40, 511, 2, 0, 9]
+
+
+@pytest.mark.parametrize("out", [BF16, F32])
+@pytest.mark.parametrize("n_in,n_out,unused", [(72, 8200, 0), (8200, 72, 300), (264, 9000, 1), (128, 8192, 77),
+                                               (9000, 24, 0), (4104, 520, 13)])
+def test_many_tiles(ctx, n_in, n_out, unused, out):
+    """Enough tiles that each block walks several, of groups with few rows and many."""
+    check_all(ctx, MANY, n_in, n_out, unused, out=out, seed=n_in)
+
+
+def test_many_tiles_strides_and_ends(ctx):
+    check_all(ctx, MANY, 80, 8192, 5, pad=8, offset=8)
+    check_all(ctx, MANY, 8192, 80, 5, pad=16)
+    e = torch.tensor(MANY).cumsum(0).tolist()
+    e[3], e[7], e[12] = -5, 1 << 30, 3
+    check_all(ctx, MANY, 8200, 40, want_ends=e)
+
+
+@pytest.mark.parametrize("counts,n_in,n_out,unused", [([64], 2048, 264, 0), ([1], 1024, 2048, 0), ([3, 0, 9], 4104, 72, 5),
+                                                      ([6000, 2500], 136, 200, 9), ([5000], 129, 75, 1), ([2], 4099, 33, 0),
+                                                      ([1, 2, 0, 700], 3000, 8, 0)])
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_few_tiles_with_long_contractions(ctx, counts, n_in, n_out, unused, out):
+    """Products whose contraction is done in parts and joined."""
+    check_all(ctx, counts, n_in, n_out, unused, out=out)
+    check_all(ctx, counts, n_in, n_out, unused, out=out, pad=3)
+
+
+def test_middling_tiles(ctx):
+    """Tiles of 128 and 256 in blocks of their own, whole pieces and not."""
+    for n_in, n_out in ((1024, 2048), (2000, 1040), (1030, 2045)):
+        check_all(ctx, [300, 0, 1000, 77], n_in, n_out, 3)
+    check_all(ctx, [2300], 2560, 2304, 0)
+    check_all(ctx, [700, 20, 130, 400], 648, 712, 10, out=F32)
+
+
+def test_many_groups(ctx):
+    """More groups than are sorted by size, and than a wave looks at at once."""
+    gen = torch.Generator().manual_seed(1)
+    counts = torch.randint(0, 4, (700,), generator=gen).tolist()
+    check_all(ctx, counts, 64, 264, 3)
+    check_all(ctx, counts, 264, 64, 3, ends=torch.int64)
+
+
 def test_one_gradient_at_a_time(ctx):
     from paper_2609_34162_amd import ops
     x, w, e, dy, _, dx, dw = check_all(ctx, [33, 0, 90], 64, 128)
