@@ -473,9 +473,14 @@ __global__ __launch_bounds__(64 * WM * WN) void k_grouped(GroupedArgs a) {
 
 typedef u32x4 __attribute__((aligned(2))) u32x4_any;
 
+__device__ __attribute__((aligned(16))) const uint32_t zero_piece[4] = {0, 0, 0, 0};
+
 // An operand whose rows start and end anywhere: the same tile in LDS, its 16-byte
-// pieces loaded into registers (element by element at the edges) and written there.
-template <int T, bool BY_DEPTH, int THREADS>
+// pieces loaded into registers and written there.  A piece past the tensor is loaded
+// from a piece of zeros, and a row's last, shorter one with the elements before it,
+// so that every load is the same instruction and none is waited for at a branch.
+// SHORT: a row may have fewer than 8 elements; those pieces come element by element.
+template <int T, bool BY_DEPTH, int THREADS, bool SHORT>
 struct Loose {
     static constexpr int kEach = T * kDepth * 2 / 16 / THREADS;
     static constexpr int kBytes = T * kDepth * 2;
@@ -483,47 +488,65 @@ struct Loose {
     const uint16_t *first;
     int64_t stride;
     int32_t outer;
-    u32x4 held[kEach];
 
     __device__ __forceinline__ void init(const uint16_t *first_, int64_t stride_, int64_t outer_) {
         first = first_, stride = stride_, outer = outer_ < T ? (int32_t)outer_ : T;
     }
+    // Piece j of this thread: its row (or depth), its place in the row, and the
+    // elements that it has (0 or less: none).
+    __device__ __forceinline__ void piece_of(int j, int left, int *r, int *piece, int *n) const {
+        const int q = j * THREADS + threadIdx.x;
+        *r = BY_DEPTH ? q / kPieces : q / 4;
+        const int place = BY_DEPTH ? q % kPieces : q & 3;
+        *piece = BY_DEPTH ? ((place >> 1) ^ turn<T>(*r)) * 2 + (place & 1) : place ^ (*r >> 1 & 3);
+        *n = *r < (BY_DEPTH ? left : outer) ? (BY_DEPTH ? outer : left) - *piece * 8 : 0;
+    }
     // Depths from k on, `left` of them being there.
-    __device__ __forceinline__ void load(int64_t k, int left) {
+    __device__ __forceinline__ void load(u32x4 (&held)[kEach], int64_t k, int left) const {
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            const int q = j * THREADS + threadIdx.x;
-            const int r = BY_DEPTH ? q / kPieces : q / 4;
-            const int place = BY_DEPTH ? q % kPieces : q & 3;
-            const int piece = BY_DEPTH ? ((place >> 1) ^ turn<T>(r)) * 2 + (place & 1) : place ^ (r >> 1 & 3);
-            const bool there = BY_DEPTH ? r < left : r < outer;
-            const int n = (BY_DEPTH ? outer : left) - piece * 8;  // elements from the piece's first on
+            int r, piece, n;
+            piece_of(j, left, &r, &piece, &n);
             const uint16_t *p = first + (BY_DEPTH ? (k + r) * stride : r * stride + k) + piece * 8;
-            u32x4 v = {0, 0, 0, 0};
-            if (there && n >= 8) {
-                v = *(const u32x4_any *)p;
-            } else if (there && n > 0) {
-#pragma unroll
-                for (int e = 0; e < 7; ++e)
+            if constexpr (SHORT) {
+                u32x4 v = {0, 0, 0, 0};
+                for (int e = 0; e < 8; ++e)
                     if (e < n) v[e / 2] |= (uint32_t)p[e] << (e % 2 * 16);
+                held[j] = v;
+            } else {
+                const uint16_t *from = n >= 8 ? p : n > 0 ? p - (8 - n) : (const uint16_t *)zero_piece;
+                held[j] = *(const u32x4_any *)from;
             }
-            held[j] = v;
         }
     }
-    __device__ __forceinline__ void write(char *lds) const {
+    __device__ __forceinline__ void write(const u32x4 (&held)[kEach], char *lds, int left) const {
 #pragma unroll
-        for (int j = 0; j < kEach; ++j) *(u32x4 *)(lds + (j * THREADS + threadIdx.x) * 16) = held[j];
+        for (int j = 0; j < kEach; ++j) {
+            u32x4 v = held[j];
+            if constexpr (!SHORT) {
+                int r, piece, n;
+                piece_of(j, left, &r, &piece, &n);
+                if (n > 0 && n < 8) {
+                    // the last n of the 8 elements to the front
+                    const int s = 8 - n;
+                    if (s & 4) v = u32x4{v[2], v[3], 0u, 0u};
+                    if (s & 2) v = u32x4{v[1], v[2], v[3], 0u};
+                    if (s & 1) v = u32x4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+                }
+            }
+            *(u32x4 *)(lds + (j * THREADS + threadIdx.x) * 16) = v;
+        }
     }
 };
 
-// T x T tiles, four waves; two buffers, and the next step's pieces in registers
-// while this one's products run.
-template <Mode MODE, int T>
+// T x T tiles, four waves; two buffers, and the next two steps' pieces on their way
+// to registers while this one's products run.
+template <Mode MODE, int T, bool SHORT>
 __global__ __launch_bounds__(256) void k_grouped_loose(GroupedArgs a) {
     constexpr int kTiles = T / 2 / 16;  // 16 x 16 tiles of a wave, each way
     constexpr bool kADepth = MODE == kDw, kBDepth = MODE != kForward;
-    using OpA = Loose<T, kADepth, 256>;
-    using OpB = Loose<T, kBDepth, 256>;
+    using OpA = Loose<T, kADepth, 256, SHORT>;
+    using OpB = Loose<T, kBDepth, 256, SHORT>;
     __shared__ __attribute__((aligned(1024))) char lds_a[2][OpA::kBytes], lds_b[2][OpB::kBytes];
     const Place at = place_of<MODE, T, T>(a);
     if (at.none) return;
@@ -538,28 +561,32 @@ __global__ __launch_bounds__(256) void k_grouped_loose(GroupedArgs a) {
     rb.init(wn);
     f32x4 acc[kTiles][kTiles] = {};
     const int steps = (at.depth + kDepth - 1) / kDepth;
-    if (steps > 0) {
-        oa.load(0, at.depth);
-        ob.load(0, at.depth);
-    }
-    for (int k = 0; k < steps; ++k) {
-        char *la = lds_a[k & 1], *lb = lds_b[k & 1];
-        oa.write(la);
-        ob.write(lb);
-        __syncthreads();
-        if (k + 1 < steps) {
-            oa.load((int64_t)(k + 1) * kDepth, at.depth - (k + 1) * kDepth);
-            ob.load((int64_t)(k + 1) * kDepth, at.depth - (k + 1) * kDepth);
+    u32x4 ha[2][OpA::kEach], hb[2][OpB::kEach];
+    auto load = [&](int f, int k) __attribute__((always_inline)) {
+        if (k >= steps) return;
+        oa.load(ha[f], (int64_t)k * kDepth, at.depth - k * kDepth);
+        ob.load(hb[f], (int64_t)k * kDepth, at.depth - k * kDepth);
+    };
+    load(0, 0);
+    load(1, 1);
+    for (int k0 = 0; k0 < steps; k0 += 2)
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            const int k = k0 + f;
+            if (k >= steps) break;
+            oa.write(ha[f], lds_a[f], at.depth - k * kDepth);
+            ob.write(hb[f], lds_b[f], at.depth - k * kDepth);
+            __syncthreads();
+            load(f, k + 2);
+            bf16x8 fa[kTiles], fb[kTiles];
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i) fa[i] = ra.read(lds_a[f], i), fb[i] = rb.read(lds_b[f], i);
+#pragma unroll
+            for (int i = 0; i < kTiles; ++i)
+#pragma unroll
+                for (int j = 0; j < kTiles; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
         }
-        bf16x8 fa[kTiles], fb[kTiles];
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i) fa[i] = ra.read(la, i), fb[i] = rb.read(lb, i);
-#pragma unroll
-        for (int i = 0; i < kTiles; ++i)
-#pragma unroll
-            for (int j = 0; j < kTiles; ++j)
-                acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[j], fa[i], acc[i][j], 0, 0, 0);
-    }
 #pragma unroll
     for (int i = 0; i < kTiles; ++i) {
         const int64_t m = at.m0 + wm + 16 * i + (lane & 15);
@@ -920,8 +947,11 @@ struct Way {
 // 8,192 rows, 16 groups, 1024 x 1024, 160 tiles of 256: 39 us (128: 44); 4,096 rows,
 // 8 groups, 2048 -> 1536, 120 tiles: 62 us (128: 51, 64: 76); 1,000 rows, 16 groups,
 // 2048 -> 1024, 128 tiles of 128: 32 us (64: 33); 64 rows, one group, 2048 x 2048, 16
-// tiles of 128: 19 us (64: 15).  Where even tiles of 64 are few, parts of the
-// contraction are done by blocks of their own, of 8 steps at least.
+// tiles of 128: 19 us (64: 15).  Where dw has few tiles even of 64 and many rows,
+// parts of the rows are done by blocks of their own (30,000 rows, 3 groups, 256 x 256:
+// 30 us against 89; 65,536 rows, 16 groups, 136 x 200: 48 against 71).  The other
+// products' contractions are shorter, and parts gained nothing there (16 rows over 16
+// groups, 4096 -> 1024: 32 us against 29; 64 rows, 2048 x 2048: 15 against 15).
 Way way_of(const GroupedArgs &a, Mode mode) {
     const int64_t t256 = likely_tiles(a, mode, 256), t128 = likely_tiles(a, mode, 128), t64 = likely_tiles(a, mode, 64);
     Way w{false, !tiled(a, mode), 64, 1};
@@ -932,10 +962,11 @@ Way way_of(const GroupedArgs &a, Mode mode) {
         w.tile = 256;
     } else if (t128 >= 150) {
         w.tile = 128;
-    } else if (t64 > 0 && t64 < 384) {
-        const int64_t depth = mode == kForward ? a.n_in : mode == kDx ? a.n_out : a.rows / (a.groups ? a.groups : 1);
+    } else if (mode == kDw && t64 > 0 && t64 < 384) {
+        const int64_t depth = a.rows / a.groups;
         int64_t n = 1024 / t64;
         n = n < depth / (8 * kDepth) ? n : depth / (8 * kDepth);
+        if (depth < 64 * kDepth) n = 1;
         n = n < 16 ? n : 16;
         const int64_t bytes = 4 * results_of(a, mode), room = bytes ? ((int64_t)64 << 20) / bytes : 1;
         n = n < room ? n : room;
@@ -952,7 +983,10 @@ void launch_tiled(const GroupedArgs &a, hipStream_t s) {
 template <Mode MODE, int T>
 void launch_loose(const GroupedArgs &a, hipStream_t s) {
     const dim3 grid((uint32_t)most_tiles(a, MODE, T), a.splits);
-    hipLaunchKernelGGL((k_grouped_loose<MODE, T>), grid, dim3(256), 0, s, a);
+    if (a.n_in < 8 || a.n_out < 8)
+        hipLaunchKernelGGL((k_grouped_loose<MODE, T, true>), grid, dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL((k_grouped_loose<MODE, T, false>), grid, dim3(256), 0, s, a);
 }
 
 template <Mode MODE>

@@ -114,6 +114,13 @@ def test_few_tiles_with_long_contractions(ctx, counts, n_in, n_out, unused, out)
     check_all(ctx, counts, n_in, n_out, unused, out=out, pad=3)
 
 
+@pytest.mark.parametrize("n_in,n_out", [(3, 5), (9, 131), (127, 2), (135, 71), (33, 4097)])
+@pytest.mark.parametrize("offset,pad", [(0, 0), (1, 1), (3, 6)])
+def test_ends_of_rows(ctx, n_in, n_out, offset, pad):
+    """Rows shorter than a piece, and last pieces of every length, at the ends of the tensors' memory."""
+    check_all(ctx, [31, 0, 150, 2, 33], n_in, n_out, 1, pad=pad, offset=offset)
+
+
 def test_middling_tiles(ctx):
     """Tiles of 128 and 256 in blocks of their own, whole pieces and not."""
     for n_in, n_out in ((1024, 2048), (2000, 1040), (1030, 2045)):
