@@ -66,7 +66,8 @@
 extern "C" {
 #endif
 
-/* Every entry point below is exported from libsdp.so; nothing else is. */
+/* Every entry point below is exported from libsdp.so, beside those of
+ * sdp_ops.h; nothing else is. */
 #define SDP_API __attribute__((visibility("default")))
 
 /* ---- status codes ------------------------------------------------------ */
