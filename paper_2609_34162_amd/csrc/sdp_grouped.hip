@@ -276,8 +276,8 @@ __device__ __forceinline__ void wait_and_meet() {
     asm volatile("" ::: "memory");
 }
 
-// A block's tile of C and its operands.  With splits, blockIdx.y is a part of the
-// contraction, whose product goes to the partial sums.
+// A block's tile of C and its operands.  With splits (dw only), blockIdx.y is a part
+// of the rows, whose product goes to the partial sums.
 struct Place {
     int64_t m0, m1, n0, n1;  // of C
     int32_t depth;
@@ -294,7 +294,6 @@ __device__ __forceinline__ Place place_of(const GroupedArgs &a) {
     p.none = false;
     p.f32 = MODE != kDx && a.out_f32 != 0;
     const int64_t n_in = a.n_in, n_out = a.n_out;
-    int64_t a_depth, b_depth, c_group = 0, c_all;  // elements from depth to depth; of C before this group, and in all
     if constexpr (MODE == kDw) {
         const int tm = (int)((n_out + BM - 1) / BM), tn = (int)((n_in + BN - 1) / BN);
         const int64_t id = xcd_order(blockIdx.x, gridDim.x);
@@ -307,10 +306,19 @@ __device__ __forceinline__ Place place_of(const GroupedArgs &a) {
         int64_t t0, t1;
         group_rows(a, e, &t0, &t1);
         p.depth = (int)(t1 - t0);
-        p.A = a.dy + t0 * a.y_stride + p.m0, p.sa = a_depth = a.y_stride;
-        p.B = a.x + t0 * a.x_stride + p.n0, p.sb = b_depth = a.x_stride;
-        c_group = (int64_t)e * n_out * n_in, c_all = a.groups * n_out * n_in;
+        p.A = a.dy + t0 * a.y_stride + p.m0, p.sa = a.y_stride;
+        p.B = a.x + t0 * a.x_stride + p.n0, p.sb = a.x_stride;
         p.C = (char *)a.dw, p.c_stride = n_in;
+        if (a.splits > 1) {
+            const int steps = (p.depth + kDepth - 1) / kDepth, each = (steps + a.splits - 1) / a.splits;
+            const int from = (int)blockIdx.y * each * kDepth;
+            p.depth = from < p.depth ? min(p.depth - from, each * kDepth) : 0;
+            p.A += p.depth ? from * p.sa : 0;
+            p.B += p.depth ? from * p.sb : 0;
+            p.C = (char *)(a.partials + blockIdx.y * (a.groups * n_out * n_in));
+            p.f32 = true;
+        }
+        p.C += (p.f32 ? 4 : 2) * (e * n_out * n_in);
     } else {
         const int64_t cols = MODE == kForward ? n_out : n_in;
         const int tn = (int)((cols + BN - 1) / BN);
@@ -328,29 +336,16 @@ __device__ __forceinline__ Place place_of(const GroupedArgs &a) {
         p.m0 = t.first, p.m1 = t.end;
         p.n0 = (int64_t)column * BN, p.n1 = cols;
         p.depth = empty ? 0 : MODE == kForward ? a.n_in : a.n_out;
-        a_depth = 1;
         if constexpr (MODE == kForward) {
             p.A = a.x + p.m0 * a.x_stride, p.sa = a.x_stride;
-            p.B = w + p.n0 * n_in, p.sb = n_in, b_depth = 1;
+            p.B = w + p.n0 * n_in, p.sb = n_in;
             p.C = (char *)a.y, p.c_stride = a.y_stride;
         } else {
             p.A = a.dy + p.m0 * a.y_stride, p.sa = a.y_stride;
-            p.B = w + p.n0, p.sb = b_depth = n_in;
+            p.B = w + p.n0, p.sb = n_in;
             p.C = (char *)a.dx, p.c_stride = a.dx_stride;
         }
-        c_all = a.rows * cols;
     }
-    if (a.splits > 1) {
-        const int steps = (p.depth + kDepth - 1) / kDepth, each = (steps + a.splits - 1) / a.splits;
-        const int from = (int)blockIdx.y * each * kDepth;
-        p.depth = from < p.depth ? min(p.depth - from, each * kDepth) : 0;
-        p.A += p.depth ? from * a_depth : 0;
-        p.B += p.depth ? from * b_depth : 0;
-        p.C = (char *)(a.partials + blockIdx.y * c_all);
-        p.c_stride = p.n1;
-        p.f32 = true;
-    }
-    p.C += (p.f32 ? 4 : 2) * c_group;
     return p;
 }
 
@@ -605,17 +600,16 @@ __global__ __launch_bounds__(256) void k_grouped_loose(GroupedArgs a) {
     }
 }
 
-// The partial sums of `elems` results in rows of `cols`, added in order and rounded.
-__global__ __launch_bounds__(256) void k_grouped_join(const float *partials, int splits, int64_t elems, int32_t cols,
-                                                      char *out, int64_t stride, int f32) {
+// dw from its partial sums, added in order and rounded.
+__global__ __launch_bounds__(256) void k_grouped_join(const float *partials, int splits, int64_t elems, void *dw,
+                                                      int f32) {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < elems; i += (int64_t)gridDim.x * 256) {
         float v = 0.0f;
         for (int k = 0; k < splits; ++k) v += partials[k * elems + i];
-        const int64_t row = i / cols, to = row * stride + (i - row * cols);
         if (f32)
-            ((float *)out)[to] = v;
+            ((float *)dw)[i] = v;
         else
-            store1((uint16_t *)out + to, v);
+            store1((uint16_t *)dw + i, v);
     }
 }
 
@@ -915,9 +909,7 @@ bool tiled(const GroupedArgs &a, Mode mode) {
 }
 
 int64_t columns_of(const GroupedArgs &a, Mode mode) { return mode == kForward ? a.n_out : a.n_in; }
-int64_t results_of(const GroupedArgs &a, Mode mode) {
-    return mode == kDw ? (int64_t)a.groups * a.n_out * a.n_in : a.rows * columns_of(a, mode);
-}
+int64_t weights_of(const GroupedArgs &a) { return (int64_t)a.groups * a.n_out * a.n_in; }
 
 // Tiles of t x t that a product makes if each group leaves half a row tile; and the
 // most that it can make.
@@ -968,7 +960,7 @@ Way way_of(const GroupedArgs &a, Mode mode) {
         n = n < depth / (8 * kDepth) ? n : depth / (8 * kDepth);
         if (depth < 64 * kDepth) n = 1;
         n = n < 16 ? n : 16;
-        const int64_t bytes = 4 * results_of(a, mode), room = bytes ? ((int64_t)64 << 20) / bytes : 1;
+        const int64_t bytes = 4 * weights_of(a), room = bytes ? ((int64_t)64 << 20) / bytes : 1;
         n = n < room ? n : room;
         w.splits = n > 1 ? (int)n : 1;
     }
@@ -1007,32 +999,22 @@ hipError_t launch(const GroupedArgs &args, hipStream_t s) {
         launch_tiled<MODE, 64, 2, 2, 6>(a, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || w.splits == 1) return e;
-    const int64_t elems = results_of(a, MODE), blocks = ceil_div(elems, 256);
-    char *out = (char *)(MODE == kForward ? a.y : MODE == kDx ? (void *)a.dx : a.dw);
+    const int64_t elems = weights_of(a), blocks = ceil_div(elems, 256);
     hipLaunchKernelGGL(k_grouped_join, dim3((uint32_t)(blocks < 4096 ? blocks : 4096)), dim3(256), 0, s, a.partials,
-                       w.splits, elems, (int32_t)columns_of(a, MODE), out,
-                       MODE == kForward ? a.y_stride : MODE == kDx ? a.dx_stride : (int64_t)a.n_in,
-                       MODE != kDx && a.out_f32);
+                       w.splits, elems, a.dw, a.out_f32);
     return hipGetLastError();
 }
 
 bool fits(const GroupedArgs &a, Mode mode) { return most_tiles(a, mode, way_of(a, mode).tile) <= kMaxBlocks; }
-size_t partial_bytes(const GroupedArgs &a, Mode mode) {
-    const Way w = way_of(a, mode);
-    return w.splits > 1 ? (size_t)w.splits * (size_t)results_of(a, mode) * 4 : 0;
-}
-
 }  // namespace
 
 bool grouped_fits(const GroupedArgs &a, bool forward, bool dx, bool dw) {
     return (!forward || fits(a, kForward)) && (!dx || fits(a, kDx)) && (!dw || fits(a, kDw));
 }
 
-size_t grouped_workspace(const GroupedArgs &a, bool forward, bool dx, bool dw) {
-    size_t n = forward ? partial_bytes(a, kForward) : 0;
-    if (dx && partial_bytes(a, kDx) > n) n = partial_bytes(a, kDx);
-    if (dw && partial_bytes(a, kDw) > n) n = partial_bytes(a, kDw);
-    return n;
+size_t grouped_workspace(const GroupedArgs &a, bool dw) {
+    const int splits = dw ? way_of(a, kDw).splits : 1;
+    return splits > 1 ? (size_t)splits * (size_t)weights_of(a) * 4 : 0;
 }
 
 hipError_t launch_grouped_forward(const GroupedArgs &a, hipStream_t s) { return launch<kForward>(a, s); }

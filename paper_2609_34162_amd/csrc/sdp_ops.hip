@@ -259,9 +259,9 @@ int check_grids(const char *call, const sdpops::GroupedArgs &a, bool forward, bo
     return SDP_OK;
 }
 
-// The products of a call, in the workspace where one is split.
+// The products of a call, the weights' gradients in the workspace where their rows are split.
 int run_grouped(sdp_ctx *ctx, sdpops::GroupedArgs &a, bool forward, bool dx, bool dw, hipStream_t s) {
-    const size_t bytes = sdpops::grouped_workspace(a, forward, dx, dw);
+    const size_t bytes = sdpops::grouped_workspace(a, dw);
     if (bytes > 0) {
         SDP_TRY(ensure_ops_space(ctx, bytes));
         a.partials = (float *)ctx->ops_space;

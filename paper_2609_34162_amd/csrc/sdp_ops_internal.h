@@ -59,14 +59,14 @@ struct GroupedArgs {
     int64_t rows, x_stride, y_stride, dx_stride;
     int32_t groups, n_in, n_out;
     int32_t ends64, out_f32;
-    float *partials;   // FP32 sums of parts of the contraction, where a product is split
+    float *partials;   // FP32 sums of parts of the rows, where dw is split
     int32_t splits;
 };
 
 // Whether each product's tiles fit one launch.
 bool grouped_fits(const GroupedArgs &a, bool forward, bool dx, bool dw);
-// Bytes of partial sums that the largest of the call's products needs (0: none).
-size_t grouped_workspace(const GroupedArgs &a, bool forward, bool dx, bool dw);
+// Bytes of partial sums that the call needs (0: none).
+size_t grouped_workspace(const GroupedArgs &a, bool dw);
 hipError_t launch_grouped_forward(const GroupedArgs &a, hipStream_t s);
 hipError_t launch_grouped_dx(const GroupedArgs &a, hipStream_t s);
 hipError_t launch_grouped_dw(const GroupedArgs &a, hipStream_t s);
