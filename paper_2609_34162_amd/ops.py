@@ -81,12 +81,13 @@ _TYPE_OF = {}
 
 
 def _type(t, what: str) -> int:
-    if not _TYPE_OF:
+    code = _TYPE_OF.get(t.dtype)
+    if code is None:
         _TYPE_OF.update(_types())
-    try:
-        return _TYPE_OF[t.dtype]
-    except KeyError:
-        raise ValueError(f"{what} has type {t.dtype}") from None
+        code = _TYPE_OF.get(t.dtype)
+        if code is None:
+            raise ValueError(f"{what} has type {t.dtype}")
+    return code
 
 
 def _ptr(t) -> Optional[int]:
@@ -98,14 +99,15 @@ def _want(ok: bool, text: str) -> None:
         raise ValueError(text)
 
 
+def _count(n: int, what: str) -> None:
+    # a larger one would lose its upper bits on the way into the descriptor
+    if n > 0x7fffffff:
+        raise ValueError(f"{what}: a dimension of {n} is too large")
+
+
 def _has_shape(t, shape, what: str) -> None:
     if t.shape != shape:
         raise ValueError(f"{what} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-
-
-def _last_contiguous(t, what: str) -> None:
-    if t.stride(-1) != 1 and t.shape[-1] > 1:
-        raise ValueError(f"{what}: the last dimension must be contiguous")
 
 
 def _dense(t, shape, what: str) -> Optional[int]:
@@ -119,54 +121,73 @@ def _dense(t, shape, what: str) -> Optional[int]:
 
 
 def _same_type(t, code: int, what: str) -> None:
-    if t is not None and _type(t, what) != code:
+    if t is not None and _TYPE_OF.get(t.dtype) != code and _type(t, what) != code:
         raise ValueError(f"{what} has another type than expected")
 
 
 def _row_stride(t, shape, what: str) -> int:
     _has_shape(t, shape, what)
-    _last_contiguous(t, what)
-    return t.stride(0)
+    strides = t.stride()
+    if strides[1] != 1 and shape[1] > 1:
+        raise ValueError(f"{what}: the last dimension must be contiguous")
+    return strides[0]
 
 
 def _heads(t, shape, what: str) -> sdp_heads:
     """[batch, tokens, heads, head_dim], or [tokens, heads, head_dim] of one sequence."""
-    if t.dim() == 3:
+    strides = t.stride()
+    if len(strides) == 3:
         t = t.unsqueeze(0)
-    _has_shape(t, shape, what)
-    _last_contiguous(t, what)
-    return sdp_heads(t.data_ptr(), *t.stride()[:3])
+        strides = t.stride()
+    if t.shape != shape:
+        _has_shape(t, shape, what)
+    if strides[3] != 1 and shape[3] > 1:
+        raise ValueError(f"{what}: the last dimension must be contiguous")
+    return sdp_heads(t.data_ptr(), strides[0], strides[1], strides[2])
+
+
+def _heads_shape(t):
+    shape = t.shape
+    if len(shape) == 4:
+        return shape
+    _want(len(shape) == 3, "q and k must be [batch, tokens, heads, head_dim]")
+    return (1, *shape)
 
 
 def _qk_desc(q, k, cos, sin, q_weight, k_weight, positions, eps, interleaved):
-    def shape(t):
-        _want(t.dim() in (3, 4), "q and k must be [batch, tokens, heads, head_dim]")
-        return (1, *t.shape) if t.dim() == 3 else tuple(t.shape)
-    qs, ks = shape(q), shape(k)
-    if qs[:2] != ks[:2] or qs[3] != ks[3]:
-        raise ValueError(f"q {qs} and k {ks} differ in batch, tokens or head_dim")
+    qs, ks = _heads_shape(q), _heads_shape(k)
+    batch, tokens, q_heads, dim = qs
+    k_batch, k_tokens, k_heads, k_dim = ks
+    if batch != k_batch or tokens != k_tokens or dim != k_dim:
+        raise ValueError(f"q {tuple(qs)} and k {tuple(ks)} differ in batch, tokens or head_dim")
+    _count(max(batch, tokens, q_heads, k_heads, dim), "q and k")
     code = _type(q, "q")
     _same_type(k, code, "k")
-    d = sdp_qk_norm_rope_desc()
-    d.type, d.batch, d.tokens, d.q_heads, d.k_heads, d.head_dim = code, qs[0], qs[1], qs[2], ks[2], qs[3]
-    weights = [w for w in (q_weight, k_weight) if w is not None]
-    d.weight_type = _type(weights[0], "a weight") if weights else SDP_TYPE_F32
-    for w in weights:
-        _same_type(w, d.weight_type, "a weight")
-    d.q_weight, d.k_weight = _dense(q_weight, (qs[3],), "q_weight"), _dense(k_weight, (qs[3],), "k_weight")
-    d.eps, d.interleaved = eps, int(bool(interleaved))
+    some = k_weight if q_weight is None else q_weight
+    weight_type = SDP_TYPE_F32 if some is None else _type(some, "a weight")
+    _same_type(k_weight, weight_type, "a weight")
+    shape = (dim,)
+    rows = rotary = 0
     if cos is not None:
-        _want(cos.dim() == 2 and sin is not None, "cos and sin must be [table_rows, rotary_dim / 2]")
+        table = cos.shape
+        _want(len(table) == 2 and sin is not None, "cos and sin must be [table_rows, rotary_dim / 2]")
         _same_type(cos, SDP_TYPE_F32, "cos")
         _same_type(sin, SDP_TYPE_F32, "sin")
-        d.table_rows, d.rotary_dim = cos.shape[0], 2 * cos.shape[1]
-        d.cos, d.sin = _dense(cos, cos.shape, "cos"), _dense(sin, cos.shape, "sin")
-    d.position_type = SDP_TYPE_I32
+        rows, rotary = table[0], 2 * table[1]
+        _count(rotary, "cos")
+        cos, sin = _dense(cos, table, "cos"), _dense(sin, table, "sin")
+    else:
+        sin = None
+    at, position_type = None, SDP_TYPE_I32
     if positions is not None:
-        d.position_type = _type(positions, "positions")
-        _want(positions.numel() == qs[0] * qs[1] and positions.is_contiguous(),
+        position_type = _type(positions, "positions")
+        _want(positions.numel() == batch * tokens and positions.is_contiguous(),
               "positions must be [batch, tokens], contiguous")
-        d.positions = positions.data_ptr()
+        at = positions.data_ptr()
+    # in the fields' order: several times as fast as setting them one by one
+    d = sdp_qk_norm_rope_desc(code, weight_type, batch, tokens, q_heads, k_heads, dim, rotary, 1 if interleaved else 0,
+                              position_type, eps, rows, cos, sin, at, _dense(q_weight, shape, "q_weight"),
+                              _dense(k_weight, shape, "k_weight"))
     return d, qs, ks
 
 
@@ -175,99 +196,99 @@ def _qk_desc(q, k, cos, sin, q_weight, k_weight, positions, eps, interleaved):
 def sdp_qk_norm_rope(ctx, q, k, q_out, k_out, cos=None, sin=None, *, q_weight=None, k_weight=None, positions=None,
                      eps: float = 1e-6, interleaved: bool = False, stream=None) -> None:
     d, qs, ks = _qk_desc(q, k, cos, sin, q_weight, k_weight, positions, eps, interleaved)
-    for t, n in ((q_out, "q_out"), (k_out, "k_out")):
-        _same_type(t, d.type, n)
-    _check(_lib.sdp_qk_norm_rope(ctx, ctypes.byref(d), ctypes.byref(_heads(q, qs, "q")),
-                                 ctypes.byref(_heads(k, ks, "k")), ctypes.byref(_heads(q_out, qs, "q_out")),
-                                 ctypes.byref(_heads(k_out, ks, "k_out")), _stream(stream)))
+    code = d.type
+    _same_type(q_out, code, "q_out")
+    _same_type(k_out, code, "k_out")
+    # (a structure passed for a pointer to one goes by reference)
+    _check(_lib.sdp_qk_norm_rope(ctx, d, _heads(q, qs, "q"), _heads(k, ks, "k"), _heads(q_out, qs, "q_out"),
+                                 _heads(k_out, ks, "k_out"), _stream(stream)))
 
 
 def sdp_qk_norm_rope_backward(ctx, q, k, dq_out, dk_out, dq, dk, cos=None, sin=None, *, q_weight=None, k_weight=None,
                               dq_weight=None, dk_weight=None, positions=None, eps: float = 1e-6,
                               interleaved: bool = False, stream=None) -> None:
     d, qs, ks = _qk_desc(q, k, cos, sin, q_weight, k_weight, positions, eps, interleaved)
-    for t, n in ((dq_out, "dq_out"), (dk_out, "dk_out"), (dq, "dq"), (dk, "dk")):
-        _same_type(t, d.type, n)
-    grads = [w for w in (dq_weight, dk_weight) if w is not None]
-    if grads and q_weight is None and k_weight is None:
-        d.weight_type = _type(grads[0], "a weight gradient")
-    for w in grads:
-        _same_type(w, d.weight_type, "a weight gradient")
+    code = d.type
+    _same_type(dq_out, code, "dq_out")
+    _same_type(dk_out, code, "dk_out")
+    _same_type(dq, code, "dq")
+    _same_type(dk, code, "dk")
+    some = dk_weight if dq_weight is None else dq_weight
+    if some is not None:
+        if q_weight is None and k_weight is None:
+            d.weight_type = _type(some, "a weight gradient")
+        _same_type(some, d.weight_type, "a weight gradient")
+        _same_type(dk_weight, d.weight_type, "a weight gradient")
+    shape = (qs[3],)
     _check(_lib.sdp_qk_norm_rope_backward(
-        ctx, ctypes.byref(d), ctypes.byref(_heads(q, qs, "q")), ctypes.byref(_heads(k, ks, "k")),
-        ctypes.byref(_heads(dq_out, qs, "dq_out")), ctypes.byref(_heads(dk_out, ks, "dk_out")),
-        ctypes.byref(_heads(dq, qs, "dq")), ctypes.byref(_heads(dk, ks, "dk")),
-        _dense(dq_weight, (qs[3],), "dq_weight"), _dense(dk_weight, (qs[3],), "dk_weight"), _stream(stream)))
+        ctx, d, _heads(q, qs, "q"), _heads(k, ks, "k"), _heads(dq_out, qs, "dq_out"), _heads(dk_out, ks, "dk_out"),
+        _heads(dq, qs, "dq"), _heads(dk, ks, "dk"), _dense(dq_weight, shape, "dq_weight"),
+        _dense(dk_weight, shape, "dk_weight"), _stream(stream)))
 
 
-def _grouped_desc(x, w, ends, what: str):
-    if x.dim() != 2 or w.dim() != 3 or ends.dim() != 1:
+def _grouped_desc(rows, w, ends, out, strides, what: str):
+    """strides: of x, of y (or dy) and of dx."""
+    shape, count = w.shape, ends.shape
+    if rows.dim() != 2 or len(shape) != 3 or len(count) != 1:
         raise ValueError(f"{what}: rows must be 2-D, w [groups, out, in] and ends [groups]")
     _want(w.is_contiguous(), "w must be contiguous")
-    d = sdp_grouped_desc()
-    d.rows, d.groups, d.out_features, d.in_features = x.shape[0], w.shape[0], w.shape[1], w.shape[2]
-    d.ends, d.ends_type = _dense(ends, (w.shape[0],), "ends"), _type(ends, "ends")
-    d.out_type = SDP_TYPE_BF16
+    groups, n_out, n_in = shape
+    _count(max(shape), "w")
+    n = rows.shape[0]
     _same_type(w, SDP_TYPE_BF16, "w")
-    return d
+    x, y, dx = strides
+    _same_type(x, SDP_TYPE_BF16, "x")
+    _same_type(dx, SDP_TYPE_BF16, "dx")
+    return sdp_grouped_desc(n, groups, n_in, n_out, SDP_TYPE_BF16 if out is None else _type(out, "an output"),
+                            _type(ends, "ends"), _dense(ends, (groups,), "ends"),
+                            0 if x is None else _row_stride(x, (n, n_in), "x"), _row_stride(y, (n, n_out), "y"),
+                            0 if dx is None else _row_stride(dx, (n, n_in), "dx"))
 
 
 def sdp_grouped_matmul(ctx, x, w, ends, y, *, stream=None) -> None:
-    d = _grouped_desc(x, w, ends, "sdp_grouped_matmul")
-    _same_type(x, SDP_TYPE_BF16, "x")
-    d.x_stride = _row_stride(x, (d.rows, d.in_features), "x")
-    d.y_stride = _row_stride(y, (d.rows, d.out_features), "y")
-    d.out_type = _type(y, "y")
-    _check(_lib.sdp_grouped_matmul(ctx, ctypes.byref(d), x.data_ptr(), w.data_ptr(), y.data_ptr(), _stream(stream)))
+    d = _grouped_desc(x, w, ends, y, (x, y, None), "sdp_grouped_matmul")
+    _check(_lib.sdp_grouped_matmul(ctx, d, x.data_ptr(), w.data_ptr(), y.data_ptr(), _stream(stream)))
 
 
 def sdp_grouped_matmul_backward(ctx, x, w, ends, dy, dx=None, dw=None, *, stream=None) -> None:
     """x may be None without dw; w is always given (its shape names the products)."""
-    d = _grouped_desc(dy, w, ends, "sdp_grouped_matmul_backward")
     _same_type(dy, SDP_TYPE_BF16, "dy")
-    d.y_stride = _row_stride(dy, (d.rows, d.out_features), "dy")
-    if x is not None:
-        _same_type(x, SDP_TYPE_BF16, "x")
-        d.x_stride = _row_stride(x, (d.rows, d.in_features), "x")
-    if dx is not None:
-        _same_type(dx, SDP_TYPE_BF16, "dx")
-        d.dx_stride = _row_stride(dx, (d.rows, d.in_features), "dx")
-    if dw is not None:
-        d.out_type = _type(dw, "dw")
-        _dense(dw, w.shape, "dw")
-    _check(_lib.sdp_grouped_matmul_backward(ctx, ctypes.byref(d), _ptr(x), w.data_ptr(), dy.data_ptr(), _ptr(dx),
-                                            _ptr(dw), _stream(stream)))
+    d = _grouped_desc(dy, w, ends, dw, (x, dy, dx), "sdp_grouped_matmul_backward")
+    _check(_lib.sdp_grouped_matmul_backward(ctx, d, _ptr(x), w.data_ptr(), dy.data_ptr(), _ptr(dx),
+                                            _dense(dw, w.shape, "dw"), _stream(stream)))
 
 
 def _distill_desc(logits, teacher_logits, teacher_index, labels, temperature, distill_weight, label_weight):
-    _want(logits.dim() == 2, "logits must be [rows, vocab]")
-    d = sdp_distill_desc()
-    d.rows, d.vocab = logits.shape
-    d.logit_type, d.logits = _type(logits, "logits"), logits.data_ptr()
-    d.logit_stride = _row_stride(logits, logits.shape, "logits")
-    d.teacher_type, d.index_type = SDP_TYPE_F32, SDP_TYPE_I64
+    shape = logits.shape
+    _want(len(shape) == 2, "logits must be [rows, vocab]")
+    rows, vocab = shape
+    _count(vocab, "logits")
+    k, teacher_type, index_type = 0, SDP_TYPE_F32, SDP_TYPE_I64
+    teacher = index = label = None
     _want((teacher_logits is None) == (teacher_index is None), "teacher_logits and teacher_index go together")
     if teacher_logits is not None:
-        _want(teacher_logits.dim() == 2, "teacher_logits must be [rows, k]")
-        shape = (d.rows, teacher_logits.shape[1])
-        d.teacher_k = shape[1]
-        d.teacher_type, d.index_type = _type(teacher_logits, "teacher_logits"), _type(teacher_index, "teacher_index")
-        d.teacher_logits = _dense(teacher_logits, shape, "teacher_logits")
-        d.teacher_index = _dense(teacher_index, shape, "teacher_index")
+        given = teacher_logits.shape
+        _want(len(given) == 2, "teacher_logits must be [rows, k]")
+        k = given[1]
+        _count(k, "teacher_logits")
+        teacher_type, index_type = _type(teacher_logits, "teacher_logits"), _type(teacher_index, "teacher_index")
+        teacher = _dense(teacher_logits, (rows, k), "teacher_logits")
+        index = _dense(teacher_index, (rows, k), "teacher_index")
     if labels is not None:
         if teacher_index is not None:
-            _same_type(labels, d.index_type, "labels")
-        d.index_type = _type(labels, "labels")
-        d.labels = _dense(labels, (d.rows,), "labels")
-    d.temperature, d.distill_weight, d.label_weight = temperature, distill_weight, label_weight
-    return d
+            _same_type(labels, index_type, "labels")
+        index_type = _type(labels, "labels")
+        label = _dense(labels, (rows,), "labels")
+    return sdp_distill_desc(rows, vocab, _type(logits, "logits"), logits.data_ptr(),
+                            _row_stride(logits, shape, "logits"), k, teacher_type, index_type, teacher, index, label,
+                            temperature, distill_weight, label_weight), shape
 
 
-def _dlogits(d, dlogits):
+def _dlogits(d, shape, dlogits):
     if dlogits is None:
         return None, 0
     _same_type(dlogits, d.logit_type, "dlogits")
-    return dlogits.data_ptr(), _row_stride(dlogits, (d.rows, d.vocab), "dlogits")
+    return dlogits.data_ptr(), _row_stride(dlogits, shape, "dlogits")
 
 
 def _f32(t, shape, what: str) -> Optional[int]:
@@ -278,16 +299,17 @@ def _f32(t, shape, what: str) -> Optional[int]:
 def sdp_distill_loss(ctx, logits, loss, lse=None, *, teacher_logits=None, teacher_index=None, labels=None,
                      temperature: float = 1.0, distill_weight: float = 1.0, label_weight: float = 0.0, row_grad=None,
                      dlogits=None, stream=None) -> None:
-    d = _distill_desc(logits, teacher_logits, teacher_index, labels, temperature, distill_weight, label_weight)
-    at, stride = _dlogits(d, dlogits)
-    _check(_lib.sdp_distill_loss(ctx, ctypes.byref(d), _f32(loss, (d.rows,), "loss"), _f32(lse, (d.rows, 2), "lse"),
-                                 _f32(row_grad, (d.rows,), "row_grad"), at, stride, _stream(stream)))
+    d, shape = _distill_desc(logits, teacher_logits, teacher_index, labels, temperature, distill_weight, label_weight)
+    at, stride = _dlogits(d, shape, dlogits)
+    rows = (shape[0],)
+    _check(_lib.sdp_distill_loss(ctx, d, _f32(loss, rows, "loss"), _f32(lse, (shape[0], 2), "lse"),
+                                 _f32(row_grad, rows, "row_grad"), at, stride, _stream(stream)))
 
 
 def sdp_distill_loss_backward(ctx, logits, lse, row_grad, dlogits, *, teacher_logits=None, teacher_index=None,
                               labels=None, temperature: float = 1.0, distill_weight: float = 1.0,
                               label_weight: float = 0.0, stream=None) -> None:
-    d = _distill_desc(logits, teacher_logits, teacher_index, labels, temperature, distill_weight, label_weight)
-    at, stride = _dlogits(d, dlogits)
-    _check(_lib.sdp_distill_loss_backward(ctx, ctypes.byref(d), _f32(lse, (d.rows, 2), "lse"),
-                                          _f32(row_grad, (d.rows,), "row_grad"), at, stride, _stream(stream)))
+    d, shape = _distill_desc(logits, teacher_logits, teacher_index, labels, temperature, distill_weight, label_weight)
+    at, stride = _dlogits(d, shape, dlogits)
+    _check(_lib.sdp_distill_loss_backward(ctx, d, _f32(lse, (shape[0], 2), "lse"),
+                                          _f32(row_grad, (shape[0],), "row_grad"), at, stride, _stream(stream)))

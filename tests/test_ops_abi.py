@@ -107,3 +107,18 @@ def test_calls_without_a_context_are_refused(ops):
     with pytest.raises(ops.SdpError) as e:
         ops.sdp_qk_norm_rope(None, q, q, q, q, cos, cos)
     assert e.value.status == ops._sdp.SDP_ERR_INVALID_ARGUMENT and "context" in e.value.detail
+
+
+def test_binding_refuses_what_32_bits_do_not_hold():
+    from paper_2609_34162_amd import ops
+    torch = pytest.importorskip("torch")
+    n = (1 << 32) + 8
+    far = lambda *shape: torch.zeros(1, dtype=torch.bfloat16).expand(*shape)
+    logits, one, ends = far(1, n), torch.zeros(1), torch.zeros(1, dtype=torch.int32)
+    with pytest.raises(ValueError, match="logits: a dimension"):
+        ops.sdp_distill_loss(None, logits, one, labels=torch.zeros(1, dtype=torch.int64))
+    w = torch.empty((1, 0, n), dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="w: a dimension"):
+        ops.sdp_grouped_matmul(None, far(1, n), w, ends, torch.zeros(1, 0))
+    with pytest.raises(ValueError, match="q and k: a dimension"):
+        ops.sdp_qk_norm_rope(None, far(1, n, 1, 8), far(1, n, 1, 8), far(1, n, 1, 8), far(1, n, 1, 8))
