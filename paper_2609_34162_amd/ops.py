@@ -281,7 +281,7 @@ def _distill_desc(logits, teacher_logits, teacher_index, labels, temperature, di
         label = _dense(labels, (rows,), "labels")
     return sdp_distill_desc(rows, vocab, _type(logits, "logits"), logits.data_ptr(),
                             _row_stride(logits, shape, "logits"), k, teacher_type, index_type, teacher, index, label,
-                            temperature, distill_weight, label_weight), shape
+                            temperature, distill_weight, label_weight)
 
 
 def _dlogits(d, shape, dlogits):
@@ -299,7 +299,8 @@ def _f32(t, shape, what: str) -> Optional[int]:
 def sdp_distill_loss(ctx, logits, loss, lse=None, *, teacher_logits=None, teacher_index=None, labels=None,
                      temperature: float = 1.0, distill_weight: float = 1.0, label_weight: float = 0.0, row_grad=None,
                      dlogits=None, stream=None) -> None:
-    d, shape = _distill_desc(logits, teacher_logits, teacher_index, labels, temperature, distill_weight, label_weight)
+    d = _distill_desc(logits, teacher_logits, teacher_index, labels, temperature, distill_weight, label_weight)
+    shape = logits.shape
     at, stride = _dlogits(d, shape, dlogits)
     rows = (shape[0],)
     _check(_lib.sdp_distill_loss(ctx, d, _f32(loss, rows, "loss"), _f32(lse, (shape[0], 2), "lse"),
@@ -309,7 +310,8 @@ def sdp_distill_loss(ctx, logits, loss, lse=None, *, teacher_logits=None, teache
 def sdp_distill_loss_backward(ctx, logits, lse, row_grad, dlogits, *, teacher_logits=None, teacher_index=None,
                               labels=None, temperature: float = 1.0, distill_weight: float = 1.0,
                               label_weight: float = 0.0, stream=None) -> None:
-    d, shape = _distill_desc(logits, teacher_logits, teacher_index, labels, temperature, distill_weight, label_weight)
+    d = _distill_desc(logits, teacher_logits, teacher_index, labels, temperature, distill_weight, label_weight)
+    shape = logits.shape
     at, stride = _dlogits(d, shape, dlogits)
     _check(_lib.sdp_distill_loss_backward(ctx, d, _f32(lse, (shape[0], 2), "lse"),
                                           _f32(row_grad, (shape[0],), "row_grad"), at, stride, _stream(stream)))
