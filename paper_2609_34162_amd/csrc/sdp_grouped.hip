@@ -671,8 +671,10 @@ __global__ __launch_bounds__(256) void k_grouped_join(const float *partials, int
 // 256 x 256 tiles, one block to a compute unit, each block walking its share of the
 // tiles as one stream of steps: the last steps of a tile load the first ones of
 // the next, and a tile's results are stored while the next one's products run.
-// (Tile by tile, with a launch of one block each, the fixed cost of a tile was 15 us,
-// next to 28 us for a contraction of 1,024.)
+// 65,536 rows, 128 groups of unequal sizes, 2048 x 1536: forward 480 us, dx 470, dw 550
+// (860, 880 and 750 TFLOP/s); forward the matrix units are busy for 42% of the time, at
+// the 2.05 GHz that the card's power leaves; the rest is weights that come from memory
+// and part tiles at the groups' ends.
 constexpr int kStreamBlocks = 256, kStreamTile = 256, kStreamWm = 2, kStreamWn = 4, kStreamNb = 4;
 constexpr int kSortedGroups = 256;  // dw: up to so many groups are taken largest first
 
@@ -994,27 +996,34 @@ struct Way {
 };
 
 // The largest tile that still occupies the 256 compute units, as it loads the fewest
-// bytes for its products.  From 256 tiles of 256 on and with two groups or more they
-// are walked as a stream, which also evens out groups of different sizes (16,384 rows,
-// 8 groups, 2048 x 2048, dw: 166 us against 199 in blocks of one tile; 65,536 rows,
-// 64 groups, 2048 x 1536: 513 against 591); one group alone fares better in blocks
-// (4096^2 x 8192, dw: 209 us against 249).  Measured with weights from memory:
-// 8,192 rows, 16 groups, 1024 x 1024, 160 tiles of 256: 39 us (128: 44); 4,096 rows,
-// 8 groups, 2048 -> 1536, 120 tiles: 62 us (128: 51, 64: 76); 1,000 rows, 16 groups,
-// 2048 -> 1024, 128 tiles of 128: 32 us (64: 33); 64 rows, one group, 2048 x 2048, 16
-// tiles of 128: 19 us (64: 15).  Where dw has few tiles even of 64 and many rows,
-// parts of the rows are done by blocks of their own (30,000 rows, 3 groups, 256 x 256:
-// 30 us against 89; 65,536 rows, 16 groups, 136 x 200: 48 against 71).  The other
-// products' contractions are shorter, and parts gained nothing there (16 rows over 16
-// groups, 4096 -> 1024: 32 us against 29; 64 rows, 2048 x 2048: 15 against 15).
+// bytes for its products.  Measured with weights from memory, 256 against 128 against
+// 64: 8,192 rows, 16 groups, 1024 x 1024, 160 tiles of 256: 36 us, 43, 57; 4,096 rows, 8
+// groups, 2048 -> 1536, 120 tiles: 59, 48, 76; 1,000 rows, 16 groups, 2048 -> 1024, 128
+// tiles of 128: 31 us (64: 33); 64 rows, one group, 2048 x 2048, 16 tiles of 128: 18 (64: 15).
+//
+// From 256 tiles of 256 on and with two groups or more they are walked as a stream.
+// It evens out the groups' sizes in dw (16,384 rows, 8 groups of unequal sizes, 2048 x
+// 2048: 163 us against 191 in blocks of one tile; 65,536 rows, 64 groups, 2048 x 1536:
+// 466 against 500; with equal groups 136 against 123 and 464 against 410, which the
+// host cannot see), and in the other products it hides the short contractions' ends
+// (65,536 rows, 128 groups, 768 -> 2048: 278 us against 333).  Long ones of large groups
+// fare better in blocks, whose tiles come to a compute unit as it gets free (16,384
+// rows, 8 groups, 2048 x 2048: 169 us against 190; 40,000 rows, 4 groups, 4096 x 4096:
+// 1101 against 1154; at 512 rows a group, 2048 -> 1536: 490 against 480).
+//
+// Where dw has few tiles even of 64 and many rows, parts of the rows are done by blocks
+// of their own (30,000 rows, 3 groups, 256 x 256: 29 us against 90; 65,536 rows, 16
+// groups, 136 x 200: 46 against 73).  The other products' contractions are shorter, and
+// parts gained nothing there (16 rows over 16 groups, 4096 -> 1024: 32 us against 29; 64
+// rows, 2048 x 2048: 15 against 15).
 Way way_of(const GroupedArgs &a, Mode mode) {
     const int64_t t256 = likely_tiles(a, mode, 256), t128 = likely_tiles(a, mode, 128), t64 = likely_tiles(a, mode, 64);
     Way w{false, !tiled(a, mode), 64, 1};
-    if (!w.loose && a.groups >= 2 && t256 >= (mode == kDw ? 257 : 256)) {
-        w.stream = true;
+    const bool long_large = mode != kDw && (mode == kForward ? a.n_in : a.n_out) >= 2048 &&
+                            a.rows >= 768 * (int64_t)a.groups;
+    if (!w.loose && t256 >= 150) {
         w.tile = 256;
-    } else if (!w.loose && t256 >= 150) {
-        w.tile = 256;
+        w.stream = a.groups >= 2 && t256 >= (mode == kDw ? 257 : 256) && !long_large;
     } else if (t128 >= 150) {
         w.tile = 128;
     } else if (mode == kDw && t64 > 0 && t64 < 384) {
