@@ -24,8 +24,9 @@
  *    so; other overlaps are refused.
  *  - Every call is asynchronous on `stream`.  Calls that use the context's
  *    workspace (sdp_qk_norm_rope_backward with weight gradients, the
- *    distillation loss where a row is split over blocks, grouped products of
- *    few tiles) order themselves after the context's last such call, whatever
+ *    distillation loss where a row is split over blocks, gradients of
+ *    few experts' weights, grouped products of sizes or strides without whole
+ *    16-byte pieces) order themselves after the context's last such call, whatever
  *    its stream; a workspace that has to grow waits for the device.
  *  - Sums, norms, softmax statistics and products are held in FP32 and an
  *    output is rounded once, to nearest even.  No atomics: the same inputs

@@ -666,6 +666,54 @@ __global__ __launch_bounds__(256) void k_grouped_join(const float *partials, int
     }
 }
 
+// ---- sizes and strides without whole pieces, laid out anew ---------------------------
+
+// Groups of rows of `src_cols` elements into groups of rows of `dst_cols`, zeros where
+// the source has no row or column: into whole pieces before the products, and out of
+// them after.  A block takes `rows` rows, a thread 16 bytes at a time.
+struct RowsCopy {
+    const void *src;
+    void *dst;
+    int64_t src_stride, dst_stride, dst_rows;  // dst_rows: of all groups
+    int32_t src_group, dst_group;              // rows of a group
+    int32_t src_cols, dst_cols, rows;
+};
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_grouped_copy(RowsCopy c) {
+    constexpr int kN = 16 / (int)sizeof(T);
+    const int pieces = (c.dst_cols - 1) / kN + 1;
+    const int64_t first = (int64_t)blockIdx.x * c.rows;
+    const int rows = (int)min((int64_t)c.rows, c.dst_rows - first);
+    for (uint32_t i = threadIdx.x; i < (uint32_t)rows * pieces; i += 256) {
+        const uint32_t r = i / pieces, piece = i - r * pieces;
+        const int64_t row = first + r, group = row / c.dst_group;
+        const int in_group = (int)(row - group * c.dst_group), col = (int)piece * kN;
+        const T *from = (const T *)c.src + (group * c.src_group + in_group) * c.src_stride + col;
+        T *to = (T *)c.dst + row * c.dst_stride + col;
+        const int n_src = in_group < c.src_group ? c.src_cols - col : 0, n_dst = c.dst_cols - col;
+        union {
+            u32x4 all;
+            T each[kN];
+        } v;
+        v.all = u32x4{0, 0, 0, 0};
+        if (n_src >= kN) {
+            v.all = *(const u32x4_any *)from;
+        } else {
+#pragma unroll
+            for (int e = 0; e < kN; ++e)
+                if (e < n_src) v.each[e] = from[e];
+        }
+        if (n_dst >= kN) {
+            *(u32x4_any *)to = v.all;
+        } else {
+#pragma unroll
+            for (int e = 0; e < kN; ++e)
+                if (e < n_dst) to[e] = v.each[e];
+        }
+    }
+}
+
 // ---- many tiles --------------------------------------------------------------------
 
 // 256 x 256 tiles, one block to a compute unit, each block walking its share of the
@@ -1077,20 +1125,136 @@ hipError_t launch(const GroupedArgs &args, hipStream_t s) {
     return hipGetLastError();
 }
 
+// A call whose tensors are laid out anew for the tiled kernels: `to`, the call on the
+// copies in the workspace (from its start; offsets until `base` is added).
+struct Packed {
+    bool any, x, w, dy, y, dx, dw;
+    GroupedArgs to;
+    size_t bytes;
+};
+
+// Which tensors have no whole pieces, and whether copies of them pay.  The loose kernel
+// does 200 to 300 TFLOP/s and the tiled ones 500 to 900, and copies go at 5 TB/s and cost
+// a launch each: they pay from some 110 operations for each byte that they move on.
+// Both products of the backward, copies against none: 65,536 rows, 16 groups, 515 x
+// 1025 (157 operations a byte for one product): 493 us against 700; 30,000 rows, 8 groups,
+// 1023 x 2047 (288): 483 against 816.  dx alone of 57,617 rows, 105 groups, 328 x 2905
+// (102): 451 against 338; forward of 8,192 rows, 32 groups, 1021 x 2047 (93): 175 against 142.
+Packed pack_of(const GroupedArgs &a, bool forward, bool dx, bool dw) {
+    Packed p{};
+    p.to = a;
+    GroupedArgs &b = p.to;
+    const int64_t n_in = ceil_div(a.n_in, 8) * 8, n_out = ceil_div(a.n_out, 8) * 8;
+    if (n_in >= (int64_t)1 << 21 || n_out >= (int64_t)1 << 21) return p;
+    b.n_in = (int32_t)n_in, b.n_out = (int32_t)n_out;
+    const bool same = n_in == a.n_in && n_out == a.n_out;
+    const bool use_x = forward || dw, use_w = forward || dx, use_dy = dx || dw;
+    const int out = a.out_f32 ? 4 : 2;
+    auto result = [&](const void *c, int64_t stride, bool cols) {
+        return !(cols && (uintptr_t)c % 16 == 0 && stride % 4 == 0 && stride < ((int64_t)1 << 21));
+    };
+    p.x = use_x && !pieces(a.x, a.x_stride, a.n_in);
+    p.dy = use_dy && !pieces(a.dy, a.y_stride, a.n_out);
+    p.w = use_w && !(same && (uintptr_t)a.w % 16 == 0);
+    p.y = forward && result(a.y, a.y_stride, n_out == a.n_out);
+    p.dx = dx && result(a.dx, a.dx_stride, n_in == a.n_in);
+    p.dw = dw && result(a.dw, a.n_in, same);
+    if (!(p.x || p.dy || p.w || p.y || p.dx || p.dw)) return p;
+    size_t at = 0;
+    int64_t moved = 0;
+    auto place = [&](bool on, int64_t elems, int size) {
+        const size_t here = at;
+        if (on) at += ((size_t)elems * size + 255) / 256 * 256, moved += 2 * elems * size;
+        return (uintptr_t)here;
+    };
+    const uintptr_t x = place(p.x, a.rows * n_in, 2), dy = place(p.dy, a.rows * n_out, 2);
+    const uintptr_t w = place(p.w, a.groups * n_out * n_in, 2), y = place(p.y, a.rows * n_out, out);
+    const uintptr_t gx = place(p.dx, a.rows * n_in, 2), gw = place(p.dw, a.groups * n_out * n_in, out);
+    const double flops = 2.0 * a.rows * a.n_in * a.n_out * ((forward ? 1 : 0) + (dx ? 1 : 0) + (dw ? 1 : 0));
+    if (p.x) b.x = (const uint16_t *)x, b.x_stride = n_in;
+    if (p.dy) b.dy = (const uint16_t *)dy;
+    if (p.w) b.w = (const uint16_t *)w;
+    if (p.y) b.y = (void *)y;
+    if (p.dx) b.dx = (uint16_t *)gx, b.dx_stride = n_in;
+    if (p.dw) b.dw = (void *)gw;
+    if (p.dy || p.y) b.y_stride = n_out;
+    p.bytes = at;
+    const bool large = (!forward || way_of(b, kForward).tile >= 128) && (!dx || way_of(b, kDx).tile >= 128) &&
+                       (!dw || way_of(b, kDw).tile >= 128);
+    p.any = large && flops > 110.0 * (double)moved + 5e9 && at <= ((size_t)2 << 30);
+    return p;
+}
+
+template <typename T>
+hipError_t copy_rows(const void *src, int64_t src_stride, int64_t src_group, int64_t src_cols, void *dst,
+                     int64_t dst_stride, int64_t dst_group, int64_t dst_cols, int64_t groups, hipStream_t s) {
+    RowsCopy c{src, dst, src_stride, dst_stride, groups * dst_group, (int32_t)src_group, (int32_t)dst_group,
+               (int32_t)src_cols, (int32_t)dst_cols, 1};
+    if (c.dst_rows == 0) return hipSuccess;
+    // a thread does a few pieces, and there are some blocks for each compute unit
+    const int64_t most = ceil_div(c.dst_rows, 2048);
+    c.rows = (int32_t)(most < 32 ? most : 32);
+    hipLaunchKernelGGL((k_grouped_copy<T>), dim3((uint32_t)ceil_div(c.dst_rows, c.rows)), dim3(256), 0, s, c);
+    return hipGetLastError();
+}
+
+hipError_t copy_out(bool f32, const void *src, int64_t src_stride, int64_t src_group, int64_t src_cols, void *dst,
+                    int64_t dst_stride, int64_t dst_group, int64_t dst_cols, int64_t groups, hipStream_t s) {
+    return f32 ? copy_rows<float>(src, src_stride, src_group, src_cols, dst, dst_stride, dst_group, dst_cols, groups, s)
+               : copy_rows<uint16_t>(src, src_stride, src_group, src_cols, dst, dst_stride, dst_group, dst_cols, groups, s);
+}
+
 bool fits(const GroupedArgs &a, Mode mode) { return most_tiles(a, mode, way_of(a, mode).tile) <= kMaxBlocks; }
 }  // namespace
 
 bool grouped_fits(const GroupedArgs &a, bool forward, bool dx, bool dw) {
-    return (!forward || fits(a, kForward)) && (!dx || fits(a, kDx)) && (!dw || fits(a, kDw));
+    const Packed p = pack_of(a, forward, dx, dw);
+    const GroupedArgs &b = p.any ? p.to : a;
+    return (!forward || fits(b, kForward)) && (!dx || fits(b, kDx)) && (!dw || fits(b, kDw));
 }
 
-size_t grouped_workspace(const GroupedArgs &a, bool dw) {
+size_t grouped_workspace(const GroupedArgs &a, bool forward, bool dx, bool dw) {
+    const Packed p = pack_of(a, forward, dx, dw);
+    if (p.any) return p.bytes;
     const int splits = dw ? way_of(a, kDw).splits : 1;
     return splits > 1 ? (size_t)splits * (size_t)weights_of(a) * 4 : 0;
 }
 
-hipError_t launch_grouped_forward(const GroupedArgs &a, hipStream_t s) { return launch<kForward>(a, s); }
-hipError_t launch_grouped_dx(const GroupedArgs &a, hipStream_t s) { return launch<kDx>(a, s); }
-hipError_t launch_grouped_dw(const GroupedArgs &a, hipStream_t s) { return launch<kDw>(a, s); }
+#define GROUPED_TRY(e)                              \
+    do {                                            \
+        const hipError_t e_ = (e);                  \
+        if (e_ != hipSuccess) return e_;            \
+    } while (0)
+
+hipError_t launch_grouped(const GroupedArgs &a, bool forward, bool dx, bool dw, void *space, hipStream_t s) {
+    const Packed p = pack_of(a, forward, dx, dw);
+    GroupedArgs b = a;
+    if (p.any) {
+        b = p.to;
+        char *base = (char *)space;
+        if (p.x) b.x = (const uint16_t *)(base + (uintptr_t)b.x);
+        if (p.dy) b.dy = (const uint16_t *)(base + (uintptr_t)b.dy);
+        if (p.w) b.w = (const uint16_t *)(base + (uintptr_t)b.w);
+        if (p.y) b.y = base + (uintptr_t)b.y;
+        if (p.dx) b.dx = (uint16_t *)(base + (uintptr_t)b.dx);
+        if (p.dw) b.dw = base + (uintptr_t)b.dw;
+        if (p.x) GROUPED_TRY(copy_rows<uint16_t>(a.x, a.x_stride, a.rows, a.n_in, (void *)b.x, b.n_in, a.rows, b.n_in, 1, s));
+        if (p.dy)
+            GROUPED_TRY(copy_rows<uint16_t>(a.dy, a.y_stride, a.rows, a.n_out, (void *)b.dy, b.n_out, a.rows, b.n_out, 1, s));
+        if (p.w)
+            GROUPED_TRY(copy_rows<uint16_t>(a.w, a.n_in, a.n_out, a.n_in, (void *)b.w, b.n_in, b.n_out, b.n_in, a.groups, s));
+    } else {
+        b.partials = (float *)space;
+    }
+    if (forward) GROUPED_TRY(launch<kForward>(b, s));
+    if (dx) GROUPED_TRY(launch<kDx>(b, s));
+    if (dw) GROUPED_TRY(launch<kDw>(b, s));
+    if (p.any && p.y)
+        GROUPED_TRY(copy_out(a.out_f32, b.y, b.n_out, a.rows, b.n_out, a.y, a.y_stride, a.rows, a.n_out, 1, s));
+    if (p.any && p.dx) GROUPED_TRY(copy_out(false, b.dx, b.n_in, a.rows, b.n_in, a.dx, a.dx_stride, a.rows, a.n_in, 1, s));
+    if (p.any && p.dw)
+        GROUPED_TRY(copy_out(a.out_f32, b.dw, b.n_in, b.n_out, b.n_in, a.dw, a.n_in, a.n_out, a.n_in, a.groups, s));
+    return hipSuccess;
+}
 
 }  // namespace sdpops

@@ -259,17 +259,14 @@ int check_grids(const char *call, const sdpops::GroupedArgs &a, bool forward, bo
     return SDP_OK;
 }
 
-// The products of a call, the weights' gradients in the workspace where their rows are split.
-int run_grouped(sdp_ctx *ctx, sdpops::GroupedArgs &a, bool forward, bool dx, bool dw, hipStream_t s) {
-    const size_t bytes = sdpops::grouped_workspace(a, dw);
+// The products of a call, with the workspace that they need.
+int run_grouped(sdp_ctx *ctx, const sdpops::GroupedArgs &a, bool forward, bool dx, bool dw, hipStream_t s) {
+    const size_t bytes = sdpops::grouped_workspace(a, forward, dx, dw);
     if (bytes > 0) {
         SDP_TRY(ensure_ops_space(ctx, bytes));
-        a.partials = (float *)ctx->ops_space;
         SDP_TRY(ops_order(ctx, s));
     }
-    if (forward) HIP_TRY(sdpops::launch_grouped_forward(a, s));
-    if (dx) HIP_TRY(sdpops::launch_grouped_dx(a, s));
-    if (dw) HIP_TRY(sdpops::launch_grouped_dw(a, s));
+    HIP_TRY(sdpops::launch_grouped(a, forward, dx, dw, ctx->ops_space, s));
     if (bytes > 0) SDP_TRY(ops_mark(ctx, s));
     return SDP_OK;
 }

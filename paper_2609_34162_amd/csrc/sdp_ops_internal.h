@@ -65,11 +65,10 @@ struct GroupedArgs {
 
 // Whether each product's tiles fit one launch.
 bool grouped_fits(const GroupedArgs &a, bool forward, bool dx, bool dw);
-// Bytes of partial sums that the call needs (0: none).
-size_t grouped_workspace(const GroupedArgs &a, bool dw);
-hipError_t launch_grouped_forward(const GroupedArgs &a, hipStream_t s);
-hipError_t launch_grouped_dx(const GroupedArgs &a, hipStream_t s);
-hipError_t launch_grouped_dw(const GroupedArgs &a, hipStream_t s);
+// Bytes of workspace that the call needs (0: none): partial sums, or copies of tensors
+// in whole pieces.
+size_t grouped_workspace(const GroupedArgs &a, bool forward, bool dx, bool dw);
+hipError_t launch_grouped(const GroupedArgs &a, bool forward, bool dx, bool dw, void *space, hipStream_t s);
 
 // ---- distillation ----------------------------------------------------------
 

@@ -470,7 +470,7 @@ bool in_pieces(const QkArgs &a, bool bf16, bool backward) {
 // each walking its share (32,768 tokens of 48 heads of 128, BF16: 157 us; 4,096
 // blocks 176, 16,384 169), four wavefuls of rows loaded ahead (two: 159 us with
 // this split).  Backward 2,048, as each leaves a row of partial sums and holds
-// more registers (256 us; 1,024: 279; 3,072: 251, but 40 instead of 34 us on
+// more registers (256 us; 1,024: 279; half as many again: 251, but 40 instead of 34 us on
 // 4,101 tokens of 16 heads).  Non-temporal loads and stores from 256 MB on, the
 // last-level cache's size: 157 against 163 us and 256 against 274; below it they
 // cost (34 against 32 us).

@@ -185,3 +185,34 @@ def test_infinity_and_nan_stay_in_their_rows_and_groups(ctx):
         assert torch.equal(torch.isfinite(y.cpu()).all(1), rows != 25)
         assert torch.equal(torch.isfinite(dx.cpu()).all(1), rows != 70)
         assert torch.isfinite(dw[0]).all() and torch.isnan(dw[1]).all() and not torch.isfinite(dw[2]).any()
+
+
+# large enough for copies in whole pieces: every tensor without them, one side only,
+# strides or addresses alone; empty groups and rows of no group among them
+@pytest.mark.parametrize("counts,n_in,n_out,unused,pad,offset", [([3000, 0, 5190], 1021, 1033, 11, 0, 0),
+                                                                 ([1, 9000], 1024, 1027, 0, 0, 0),
+                                                                 ([9000], 1001, 1024, 200, 3, 1),
+                                                                 ([5000, 5001], 1024, 1024, 3, 5, 0),
+                                                                 ([4096, 4099], 1024, 1040, 0, 0, 3)])
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_copies_in_whole_pieces(ctx, counts, n_in, n_out, unused, pad, offset, out):
+    check_all(ctx, counts, n_in, n_out, unused=unused, out=out, pad=pad, offset=offset, seed=11)
+
+
+def test_copies_on_two_streams(ctx):
+    """Two calls that share the workspace, on streams of their own, with nothing between them."""
+    from paper_2609_34162_amd import ops
+    gen = torch.Generator().manual_seed(12)
+    ends = torch.tensor([4000, 8200], dtype=torch.int32).cuda()
+    x = [torch.randn((8200, 1021), generator=gen).to(BF16).cuda() for _ in range(2)]
+    w = torch.randn((2, 1033, 1021), generator=gen).to(BF16).cuda()
+    y = [torch.empty((8200, 1033), dtype=BF16, device="cuda") for _ in range(4)]
+    for i in range(2):
+        ops.sdp_grouped_matmul(ctx, x[i], w, ends, y[i])
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for i, s in enumerate(streams):
+        ops.sdp_grouped_matmul(ctx, x[i], w, ends, y[2 + i], stream=s)
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert torch.equal(y[i].view(torch.int16), y[2 + i].view(torch.int16))
