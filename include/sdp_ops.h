@@ -132,7 +132,9 @@ typedef struct {
 } sdp_grouped_desc;
 
 /* y[t] = x[t] w[e]^T for every row t of group e; w is [groups, out, in],
- * contiguous.  Rows of no group are set to 0. */
+ * contiguous.  Rows of no group are set to 0.  Large products of tensors without
+ * whole 16-byte pieces take copies of them in the context's workspace (up to
+ * 2 GiB, from about 110 operations for each byte copied on). */
 SDP_API int sdp_grouped_matmul(sdp_ctx *ctx, const sdp_grouped_desc *desc, const uint16_t *x, const uint16_t *w,
                                void *y, void *stream);
 

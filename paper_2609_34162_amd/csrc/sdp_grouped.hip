@@ -721,7 +721,7 @@ __global__ __launch_bounds__(256) void k_grouped_copy(RowsCopy c) {
 // the next, and a tile's results are stored while the next one's products run.
 // 65,536 rows, 128 groups of unequal sizes, 2048 x 1536: forward 480 us, dx 470, dw 550
 // (860, 880 and 750 TFLOP/s); forward the matrix units are busy for 42% of the time, at
-// the 2.05 GHz that the card's power leaves; the rest is weights that come from memory
+// the 2.1 GHz that the card's power leaves; the rest is weights that come from memory
 // and part tiles at the groups' ends.
 constexpr int kStreamBlocks = 256, kStreamTile = 256, kStreamWm = 2, kStreamWn = 4, kStreamNb = 4;
 constexpr int kSortedGroups = 256;  // dw: up to so many groups are taken largest first

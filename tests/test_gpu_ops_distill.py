@@ -225,3 +225,28 @@ def test_same_bits_again_and_on_another_stream(ctx, rows, vocab):
     for other in got[1:]:
         for a, b in zip(got[0], other):
             assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("rows,vocab", [(4, 700), (4, 151936), (600, 8000)])
+def test_rows_of_nothing_but_masked_logits(ctx, rows, vocab):
+    """NaN where the row has a label (as the definition), 0 where it has none, the other rows as ever."""
+    from paper_2609_34162_amd import ops
+    st = make(rows, vocab, 0, labels=True, seed=21)
+    z, labels = st["z"], st["labels"]
+    labels[:] = 5
+    z[1], z[2] = -INF, -INF
+    labels[2] = -100
+    z[3], labels[3] = torch.finfo(BF16).min, 7  # all alike: an even distribution
+    loss, lse, grad = torch.empty(rows, device="cuda"), torch.empty((rows, 2), device="cuda"), torch.empty_like(z)
+    for again in (False, True):
+        if again:
+            ops.sdp_distill_loss_backward(ctx, z, lse, st["row_grad"], grad, labels=labels, label_weight=1.0)
+        else:
+            ops.sdp_distill_loss(ctx, z, loss, lse, labels=labels, label_weight=1.0, row_grad=st["row_grad"], dlogits=grad)
+        assert loss[1].isnan() and loss[2] == 0
+        assert grad[1].isnan().any() and not grad[2].any()
+        rest = [r for r in range(rows) if r not in (1, 2)]
+        (rl, bl), _, (rg, bg) = ops_ref.distill(z[rest], None, None, labels[rest], 1.0, 1.0, 1.0, st["row_grad"][rest], BF16)
+        ops_ref.check(loss[rest], rl, bl, "loss")
+        ops_ref.check(grad[rest], rg, bg, "dlogits")
+        grad.fill_(7.0)
