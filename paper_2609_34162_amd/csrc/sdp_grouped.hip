@@ -458,10 +458,10 @@ __global__ __launch_bounds__(64 * WM * WN) void k_grouped(GroupedArgs a) {
         for (int k = 0; k < NB; ++k) load(bufs[k]);
         wait_and_meet<(NB - 1) * kLoads>();
         read(lds0, 0);
-        constexpr int kUnroll = NB % 2 ? 2 * NB : NB;
-        for (int k = 0; k < steps; k += kUnroll) {
+        static_assert(NB % 2 == 0, "a step's registers follow from its buffer");
+        for (int k = 0; k < steps; k += NB) {
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
+            for (int u = 0; u < NB; ++u) {
                 if (u > 0 && k + u >= steps) break;
                 step(u & 1, bufs[u % NB], bufs[(u + 1) % NB]);
             }
@@ -1061,7 +1061,9 @@ struct Way {
 //
 // Where dw has few tiles even of 64 and many rows, parts of the rows are done by blocks
 // of their own (30,000 rows, 3 groups, 256 x 256: 29 us against 90; 65,536 rows, 16
-// groups, 136 x 200: 46 against 73).  The other products' contractions are shorter, and
+// groups, 136 x 200: 46 against 73); loose tiles of 128, four waves each, want it up to
+// two a compute unit (65,536 rows, 8 groups, 261 x 1025: 280 us against 456; 16 groups,
+// 255 x 777: 175 against 307).  The other products' contractions are shorter, and
 // parts gained nothing there (16 rows over 16 groups, 4096 -> 1024: 32 us against 29; 64
 // rows, 2048 x 2048: 15 against 15).
 Way way_of(const GroupedArgs &a, Mode mode) {
@@ -1074,9 +1076,11 @@ Way way_of(const GroupedArgs &a, Mode mode) {
         w.stream = a.groups >= 2 && t256 >= (mode == kDw ? 257 : 256) && !long_large;
     } else if (t128 >= 150) {
         w.tile = 128;
-    } else if (mode == kDw && t64 > 0 && t64 < 384) {
+    }
+    const int64_t tiles = w.tile == 64 ? t64 : t128, few = w.tile == 64 ? 384 : w.loose ? 513 : 0;
+    if (mode == kDw && w.tile < 256 && tiles > 0 && tiles < few) {
         const int64_t depth = a.rows / a.groups;
-        int64_t n = 1024 / t64;
+        int64_t n = 1024 / tiles;
         n = n < depth / (8 * kDepth) ? n : depth / (8 * kDepth);
         if (depth < 64 * kDepth) n = 1;
         n = n < 16 ? n : 16;

@@ -52,7 +52,7 @@ def test_grouped_rows(ctx, stride):
     ops_ref.check(dw, rw, bw, "dw")
 
 
-# 2,100 columns a group: whole pieces, or (1,025 wide) not
+# whole pieces in every row, or (1,025 wide) not
 @pytest.mark.parametrize("n_in,n_out", [(1032, 1048), (1025, 1049)])
 def test_grouped_weights(ctx, n_in, n_out):
     from paper_2609_34162_amd import ops
