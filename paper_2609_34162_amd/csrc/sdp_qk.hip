@@ -6,7 +6,7 @@
 //   dx = r (u - x r mean(u x r)),  dw = sum over rows of dn x r
 // Every element is read once and written once: HBM bounds both directions.
 // 32,768 tokens of 48 heads of 128 in BF16, views of a fused projection: forward
-// 160 us (5.1 TB/s of the tensors' bytes), backward 255 us (4.8 TB/s); a copy of
+// 160 us (5.1 TB/s of the tensors' bytes), backward 251 us (4.8 TB/s); a copy of
 // 4 GiB reaches 4.7 to 4.8.
 #include <algorithm>
 
