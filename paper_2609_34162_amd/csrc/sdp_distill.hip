@@ -561,10 +561,11 @@ __global__ __launch_bounds__(THREADS) void k_distill_resident(DistillArgs a) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) m = top_bits(m, held[j]);
             const float own = top_of_bits(m);
-            top = block_top(own != own || !(last >= own) ? own : last, t_top, &t_top);
+            // a negative one says nothing while pieces may hold larger ones unseen
+            top = block_top(last >= 0.0f ? fmaxf(own, last) : own, t_top, &t_top);
         }
         if (kN != 8 || top == kNegInf) {
-            // 32 bits, or nothing in the row but negative values
+            // 32 bits, or no value in the row that is not negative
             top = last;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {

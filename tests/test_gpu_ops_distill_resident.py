@@ -1,0 +1,89 @@
+"""sdp_distill_loss with its gradient on enough rows that a block holds each in
+its registers, against 64-bit definitions of some of the rows: the first and
+last, those that a block takes second, and those with planted values."""
+import pytest
+
+import gpu_util
+import ops_ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+INF, LOWEST = float("inf"), torch.finfo(BF16).min
+SOME = [0, 1, 2, 3, 4, 5, 6, 7, 8, 9, 77, 190, 255, 256, 257, 299]
+ROWS = 300  # a block holds rows from 192 on; a grid of 256 blocks takes the last 44 in a second round
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    sdp = gpu_util.need_gpu()
+    c = sdp.sdp_ctx_create(0, 0, 1, 0)
+    yield c
+    torch.cuda.synchronize()
+    sdp.sdp_ctx_destroy(c)
+
+
+def make(vocab, k, dtype, rows=ROWS, labels=True, seed=0, sigma=3.0, mean=0.0):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    st = dict(z=(torch.randn((rows, vocab), generator=gen, device="cuda") * sigma + mean).to(dtype), index=None,
+              teacher=None, labels=None)
+    if k:
+        # distinct places: a step apart, from anywhere
+        first = torch.randint(0, vocab, (rows, 1), generator=gen, device="cuda")
+        at = (first + max(1, vocab // k) * torch.arange(k, device="cuda")) % vocab
+        at[torch.rand(at.shape, generator=gen, device="cuda") < 0.1] = -1
+        st["index"] = at
+        st["teacher"] = torch.randn((rows, k), generator=gen, device="cuda") * 2 + 5
+    if labels:
+        y = torch.randint(0, vocab, (rows,), generator=gen, device="cuda")
+        y[torch.rand(rows, generator=gen, device="cuda") < 0.2] = -100
+        st["labels"] = y
+    st["row_grad"] = torch.rand(rows, generator=gen, device="cuda") + 0.5
+    return st
+
+
+def bits(t):
+    return t.contiguous().view(torch.int16 if t.dtype == BF16 else torch.int32)
+
+
+def check_some(ctx, st, tau=1.0, a=1.0, b=0.5, some=SOME):
+    """Loss and gradient in one call, the gradient from its lse, and in place, on all rows; `some` of them checked."""
+    from paper_2609_34162_amd import ops
+    z = st["z"]
+    rows, vocab = z.shape
+    more = dict(teacher_logits=st["teacher"], teacher_index=st["index"], labels=st["labels"], temperature=tau,
+                distill_weight=a, label_weight=b)
+    loss, lse = torch.full((rows,), 7.0, device="cuda"), torch.full((rows, 2), 7.0, device="cuda")
+    d, back = torch.full_like(z, 7.0), torch.full_like(z, 7.0)
+    ops.sdp_distill_loss(ctx, z, loss, lse, row_grad=st["row_grad"], dlogits=d, **more)
+    ops.sdp_distill_loss_backward(ctx, z, lse, st["row_grad"], back, **more)
+    part = lambda t: None if t is None else t[some].contiguous()
+    (rl, bl), (rs, bs), (rg, bg) = ops_ref.distill(part(z), part(st["teacher"]), part(st["index"]), part(st["labels"]),
+                                                   tau, a, b, part(st["row_grad"]), z.dtype)
+    ops_ref.check(loss[some], rl, bl, "loss")
+    ops_ref.check(lse[some], rs, bs, "lse")
+    ops_ref.check(d[some], rg, bg, "dlogits")
+    ops_ref.check(back[some], rg, bg, "dlogits (backward)")
+    again, own = torch.empty_like(loss), z.clone()
+    ops.sdp_distill_loss(ctx, own, again, None, row_grad=st["row_grad"], dlogits=own, **more)
+    assert torch.equal(bits(own), bits(d)) and torch.equal(bits(again), bits(loss))
+
+
+# 8 values to a piece: rows with 1 to 7 more, in blocks of 256 and of 1,024 threads
+@pytest.mark.parametrize("vocab,tail", [(v, t) for v in (5, 1003, 8001, 40007)
+                                        for t in (-1e4, LOWEST, -INF, None, 0.0, 2.0)
+                                        if v > 8 or t not in (LOWEST, -INF)])
+@pytest.mark.parametrize("tau", [1.0, 2.0])
+def test_rows_of_negative_logits_with_a_short_last_piece(ctx, vocab, tail, tau):
+    """The largest logit is among whole pieces of nothing but negative values, the last few being other values."""
+    st = make(vocab, min(4, vocab), BF16, seed=vocab)
+    z, short = st["z"], vocab % 8
+    z[:250] = -5.0 - z[:250].abs()  # the other rows: of both signs
+    if tail is not None:
+        z[:, vocab - short:] = tail
+        if st["labels"] is not None and tail < -100:
+            # nothing is learned from the masked ones
+            st["labels"] = torch.where(st["labels"] >= vocab - short, 0, st["labels"])
+            st["index"] = torch.where(st["index"] >= vocab - short, -1, st["index"])
+    check_some(ctx, st, tau)
