@@ -493,7 +493,8 @@ __global__ __launch_bounds__(THREADS) void k_distill_resident(DistillArgs a) {
     int64_t row = blockIdx.x;
     // a thread's pieces are THREADS apart: one offset, and a scalar base for each
     const uint32_t at = (uint32_t)tid * kN;
-    // places and t / tau of a row's entries; an index past the vocabulary is kept as its size
+    // places and t / tau of a row's entries (-inf where their term is off); an index past
+    // the vocabulary is kept as its size
     auto fetch_entries = [&](int64_t of, Entries &en) __attribute__((always_inline)) {
 #pragma unroll 1
         for (int j = tid; j <= a.k; j += THREADS) {
@@ -501,7 +502,7 @@ __global__ __launch_bounds__(THREADS) void k_distill_resident(DistillArgs a) {
             float t = kNegInf;
             if (j < a.k) {
                 v = load_int(a.teacher_index, of * a.k + j, a.index64);
-                t = load_either(a.teacher_logits, of * a.k + j, a.teacher_bf16) * a.inv_tau;
+                if (teacher) t = load_either(a.teacher_logits, of * a.k + j, a.teacher_bf16) * a.inv_tau;
             } else if (labels) {
                 v = load_int(a.labels, of, a.index64);
             }

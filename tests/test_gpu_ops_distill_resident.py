@@ -87,3 +87,27 @@ def test_rows_of_negative_logits_with_a_short_last_piece(ctx, vocab, tail, tau):
             st["labels"] = torch.where(st["labels"] >= vocab - short, 0, st["labels"])
             st["index"] = torch.where(st["index"] >= vocab - short, -1, st["index"])
     check_some(ctx, st, tau)
+
+
+@pytest.mark.parametrize("rows", [4, ROWS])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("value", [float("nan"), INF, -INF])
+def test_a_weight_of_zero_leaves_the_teacher_out(ctx, rows, dtype, value):
+    """Whatever its logits hold, on few rows and on many: the bits of the call without a teacher."""
+    from paper_2609_34162_amd import ops
+    st = make(2000, 6, dtype, rows=rows, seed=3)
+    st["labels"][:4] = 5
+    st["index"][0, :], st["teacher"][0, :] = torch.arange(6, device="cuda"), value
+    st["teacher"][1, 2] = value
+    st["index"][1, 2] = 11
+    got = []
+    for with_teacher in (False, True):
+        out = (torch.empty(rows, device="cuda"), torch.empty((rows, 2), device="cuda"), torch.empty_like(st["z"]),
+               torch.empty_like(st["z"]))
+        more = dict(teacher_logits=st["teacher"], teacher_index=st["index"]) if with_teacher else {}
+        more.update(labels=st["labels"], distill_weight=0.0, label_weight=1.0, temperature=2.0)
+        ops.sdp_distill_loss(ctx, st["z"], out[0], out[1], row_grad=st["row_grad"], dlogits=out[2], **more)
+        ops.sdp_distill_loss_backward(ctx, st["z"], out[1], st["row_grad"], out[3], **more)
+        got.append(out)
+    for a, b in zip(*got):
+        assert torch.isfinite(a).all() and torch.equal(bits(a), bits(b))
