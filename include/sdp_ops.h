@@ -118,7 +118,8 @@ SDP_API int sdp_qk_norm_rope_backward(sdp_ctx *ctx, const sdp_qk_norm_rope_desc 
  * [groups], SDP_TYPE_I32 or SDP_TYPE_I64, in device memory.  A value below
  * the one before it, or past rows, is taken as that one.  Rows past the last
  * end belong to no group.  x, w, dy are BF16; out_type (SDP_TYPE_BF16 or
- * SDP_TYPE_F32) is y's and dw's. */
+ * SDP_TYPE_F32) is y's and dw's.  groups * out_features * in_features is at
+ * most 2^60. */
 typedef struct {
     int64_t rows;
     int32_t groups;

@@ -233,6 +233,8 @@ int check_grouped(const char *call, sdp_ctx *ctx, const sdp_grouped_desc *d) {
     if (d->groups < 0 || d->groups > SDP_GROUPED_MAX_GROUPS)
         return fail(SDP_ERR_INVALID_ARGUMENT, "%s: groups must be in 0..%d (got %d)", call, SDP_GROUPED_MAX_GROUPS,
                     d->groups);
+    if (sdpops::product(d->groups, d->out_features, d->in_features) < 0)
+        return fail(SDP_ERR_INVALID_ARGUMENT, "%s: groups, out_features and in_features multiply to more than 2^60", call);
     if (!is_float_type(d->out_type) || !is_int_type(d->ends_type))
         return fail(SDP_ERR_INVALID_ARGUMENT, "%s: out_type or ends_type is none of those allowed", call);
     return SDP_OK;

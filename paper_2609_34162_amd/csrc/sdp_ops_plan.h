@@ -1,6 +1,6 @@
 // Decisions of the training operators' host code that need no device, free of
-// HIP so that they can be checked without one: extents and overlaps of strided
-// tensors.
+// HIP so that they can be checked without one: sizes, extents and overlaps of
+// strided tensors.
 #pragma once
 
 #include <cstdint>
@@ -14,6 +14,13 @@ struct Layout {
     int64_t stride[3];
     int64_t inner;
 };
+
+// a b c of three sizes, or -1 where that does not fit 60 bits.
+inline int64_t product(int64_t a, int64_t b, int64_t c) {
+    if (a == 0 || b == 0 || c == 0) return 0;
+    const int64_t most = (int64_t)1 << 60;
+    return b <= most / a && c <= most / (a * b) ? a * b * c : -1;
+}
 
 inline bool no_elements(const Layout &l) { return l.inner == 0 || l.ext[0] == 0 || l.ext[1] == 0 || l.ext[2] == 0; }
 

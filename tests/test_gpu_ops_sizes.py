@@ -1,0 +1,39 @@
+"""Sizes at the edges of what the training operators take."""
+import ctypes
+
+import pytest
+
+import gpu_util
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def lib():
+    sdp = gpu_util.need_gpu()
+    from paper_2609_34162_amd import ops
+    c = sdp.sdp_ctx_create(0, 0, 1, 0)
+    yield sdp, ops, c
+    torch.cuda.synchronize()
+    sdp.sdp_ctx_destroy(c)
+
+
+@pytest.mark.parametrize("groups,n_in,n_out", [(2048, 1 << 26, 1 << 27), (64, 1 << 30, 1 << 28), (2048, 1 << 28, 1 << 28)])
+def test_weights_of_more_elements_than_64_bits_count_are_refused(lib, groups, n_in, n_out):
+    """By the host, before anything else of the description is looked at: w need not even be there."""
+    sdp, ops, ctx = lib
+    x, y = torch.zeros(8, dtype=BF16, device="cuda"), torch.full((8,), 7.0, dtype=BF16, device="cuda")
+    ends = torch.ones(groups, dtype=torch.int32, device="cuda")
+    d = ops.sdp_grouped_desc(1, groups, n_in, n_out, ops.SDP_TYPE_BF16, ops.SDP_TYPE_I32, ends.data_ptr(), 0, 0, 0)
+    for call in (lambda: sdp._lib.sdp_grouped_matmul(ctx, ctypes.byref(d), x.data_ptr(), None, y.data_ptr(), None),
+                 lambda: sdp._lib.sdp_grouped_matmul_backward(ctx, ctypes.byref(d), x.data_ptr(), None, x.data_ptr(),
+                                                              y.data_ptr(), None, None),
+                 lambda: sdp._lib.sdp_grouped_matmul_backward(ctx, ctypes.byref(d), x.data_ptr(), None, x.data_ptr(),
+                                                              None, y.data_ptr(), None)):
+        with pytest.raises(ops.SdpError, match="multiply to more than") as e:
+            sdp._check(call())
+        assert e.value.status == sdp.SDP_ERR_INVALID_ARGUMENT
+    assert (y == 7).all()
