@@ -11,6 +11,7 @@
 
 #include "sdp_ops_device.h"
 #include "sdp_ops_internal.h"
+#include "sdp_ops_plan.h"
 
 namespace sdpops {
 namespace {
@@ -346,7 +347,7 @@ __device__ __forceinline__ Place place_of(const GroupedArgs &a) {
         p.B = a.x + t0 * a.x_stride + p.n0, p.sb = a.x_stride;
         p.C = (char *)a.dw, p.c_stride = n_in;
         if (a.splits > 1) {
-            const int steps = (p.depth + kDepth - 1) / kDepth, each = (steps + a.splits - 1) / a.splits;
+            const int steps = parts_of(p.depth, kDepth), each = parts_of(steps, a.splits);
             const int from = (int)blockIdx.y * each * kDepth;
             p.depth = from < p.depth ? min(p.depth - from, each * kDepth) : 0;
             p.A += p.depth ? from * p.sa : 0;
@@ -406,7 +407,7 @@ __global__ __launch_bounds__(64 * WM * WN) void k_grouped(GroupedArgs a) {
     const int wave = wave_id(), lane = threadIdx.x & 63;
     const int wm = wave / WN * 16, wn = wave % WN * (BN / WN);
     f32x4 acc[MT][NT] = {};
-    const int steps = (at.depth + kDepth - 1) / kDepth;
+    const int steps = parts_of(at.depth, kDepth);
     // the whole contraction, over the first MU of a wave's row fragments
     auto contract = [&](auto used) __attribute__((always_inline)) {
         constexpr int MU = decltype(used)::value;
@@ -608,7 +609,7 @@ __global__ __launch_bounds__(256) void k_grouped_loose(GroupedArgs a) {
     ra.init(wm);
     rb.init(wn);
     f32x4 acc[kTiles][kTiles] = {};
-    const int steps = (at.depth + kDepth - 1) / kDepth;
+    const int steps = parts_of(at.depth, kDepth);
     u32x4 ha[2][OpA::kEach], hb[2][OpB::kEach];
     auto load = [&](int f, int k) __attribute__((always_inline)) {
         if (k >= steps) return;
@@ -927,7 +928,7 @@ __global__ __launch_bounds__(512) void k_grouped_stream(GroupedArgs a) {
 
     for (;;) {
         // whole fours: past the contraction loads bring zeros
-        const int fours = cur.depth > 0 ? (cur.depth + 4 * kDepth - 1) / (4 * kDepth) : 1;
+        const int fours = cur.depth > 0 ? parts_of(cur.depth, 4 * kDepth) : 1;
         const int64_t next_id = tile_id(round + 1);
         const bool has_next = next_id < total;
         Tile next = cur;

@@ -15,6 +15,9 @@ struct Layout {
     int64_t inner;
 };
 
+// a / b rounded up, for all a >= 0 that an int32_t holds (a + b - 1 may not).
+constexpr int32_t parts_of(int32_t a, int32_t b) { return a / b + (a % b != 0 ? 1 : 0); }
+
 // a b c of three sizes, or -1 where that does not fit 60 bits.
 inline int64_t product(int64_t a, int64_t b, int64_t c) {
     if (a == 0 || b == 0 || c == 0) return 0;

@@ -1,6 +1,8 @@
-// Sizes in sdp_ops_plan.h on the CPU: products of three sizes against 128 bits.
+// Sizes in sdp_ops_plan.h on the CPU: products of three sizes against 128 bits,
+// quotients rounded up against 64.
 #include <cstdio>
 #include <cstdlib>
+#include <initializer_list>
 
 #include "sdp_ops_plan.h"
 
@@ -21,6 +23,10 @@ int main() {
             }
     // 2^64, which is 0 in 64 bits
     EXPECT(sdpops::product(2048, 1 << 26, 1 << 27) == -1 && sdpops::product(64, 1 << 28, 1 << 30) == -1);
+    for (int64_t a : edge)
+        for (int64_t less = 0; less < 200 && less <= a; ++less)
+            for (int32_t b : {1, 3, 16, 32, 128})
+                EXPECT(sdpops::parts_of((int32_t)(a - less), b) == (a - less + b - 1) / b);
     if (!bad) std::printf("ok\n");
     return bad != 0;
 }

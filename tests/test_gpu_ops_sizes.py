@@ -37,3 +37,19 @@ def test_weights_of_more_elements_than_64_bits_count_are_refused(lib, groups, n_
             sdp._check(call())
         assert e.value.status == sdp.SDP_ERR_INVALID_ARGUMENT
     assert (y == 7).all()
+
+
+# 8 columns: whole pieces; 9: none.  Every row is the same one, read over and over.
+@pytest.mark.parametrize("n", [8, 9])
+def test_sums_over_as_many_rows_as_32_bits_count(lib, n):
+    """dw of one group: 16 parts of 2^27 rows, whose sums of ones and small powers of two are exact until their last
+    steps, each off by at most 2^-24 of the sum; then 16 additions."""
+    sdp, ops, ctx = lib
+    rows = (1 << 31) - 1
+    power = torch.arange(n, device="cuda") % 3
+    x, dy = (2.0 ** power).to(BF16).expand(rows, n), (-(2.0 ** -power)).to(BF16).expand(rows, n)
+    w = torch.zeros((1, n, n), dtype=BF16, device="cuda")
+    dw = torch.full((1, n, n), 7.0, device="cuda")
+    ops.sdp_grouped_matmul_backward(ctx, x, w, torch.tensor([rows], device="cuda"), dy, None, dw)
+    want = -float(rows) * (2.0 ** (power[None, :] - power[:, None]).double())
+    assert ((dw[0].double() - want).abs() <= 64 * 2.0 ** -24 * want.abs()).all(), dw

@@ -5,7 +5,7 @@ import subprocess
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
-def test_products_of_sizes(tmp_path):
+def test_products_and_quotients_of_sizes(tmp_path):
     exe = tmp_path / "ops_sizes_check"
     subprocess.check_call(["g++", "-std=c++17", "-O1", "-Wall", "-Werror", "-I",
                            os.path.join(ROOT, "paper_2609_34162_amd", "csrc"),
