@@ -27,7 +27,15 @@
  *    distillation loss where a row is split over blocks, gradients of
  *    few experts' weights, grouped products of sizes or strides without whole
  *    16-byte pieces) order themselves after the context's last such call, whatever
- *    its stream; a workspace that has to grow waits for the device.
+ *    its stream; a workspace that has to grow waits for the device.  It stays as
+ *    large as its largest call needed until the context is destroyed.
+ *  - A call that uses no workspace may be captured into a HIP graph: the norm and
+ *    rotation, their backward without weight gradients, sdp_distill_loss_backward,
+ *    sdp_distill_loss with dlogits where rows stay in registers (192 or more, of at
+ *    most 311,311 bytes each), grouped products of whole 16-byte pieces other than
+ *    gradients of few weights.  One that uses it is refused on a capturing stream:
+ *    the graph would keep the workspace's address past the context's next larger
+ *    call.
  *  - Sums, norms, softmax statistics and products are held in FP32 and an
  *    output is rounded once, to nearest even.  No atomics: the same inputs
  *    give the same bits.

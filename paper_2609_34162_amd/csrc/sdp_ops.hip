@@ -112,8 +112,15 @@ int ensure_ops_space(sdp_ctx *ctx, size_t bytes) {
     return SDP_OK;
 }
 
-// A call that uses the workspace runs after the last one that did.
-int ops_order(sdp_ctx *ctx, hipStream_t s) {
+// The workspace for a call, which then runs after the last one that used it.  A
+// captured graph would keep the workspace's address after it has grown, and the
+// context's event would become part of the capture, so such a call is refused.
+int take_ops_space(sdp_ctx *ctx, const char *call, size_t bytes, hipStream_t s) {
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (s) HIP_TRY(hipStreamIsCapturing(s, &capture));
+    if (capture != hipStreamCaptureStatusNone)
+        return fail(SDP_ERR_INVALID_ARGUMENT, "%s: a call that uses the context's workspace cannot be captured", call);
+    SDP_TRY(ensure_ops_space(ctx, bytes));
     if (ctx->ops_done_valid) HIP_TRY(hipStreamWaitEvent(s, ctx->ops_done, 0));
     return SDP_OK;
 }
@@ -213,10 +220,9 @@ int qk_call(sdp_ctx *ctx, const char *call, const sdp_qk_norm_rope_desc *d, cons
     sdpops::qk_split(a, bf16, backward);
     if (sums) {
         const int64_t per[2] = {(int64_t)a.blocks[0] * a.dim, (int64_t)a.blocks[1] * a.dim};
-        SDP_TRY(ensure_ops_space(ctx, (size_t)(per[0] + per[1] + 4) * 4));
+        SDP_TRY(take_ops_space(ctx, call, (size_t)(per[0] + per[1] + 4) * 4, s));
         a.side[0].partials = dweight[0] ? (float *)ctx->ops_space : nullptr;
         a.side[1].partials = dweight[1] ? (float *)ctx->ops_space + per[0] : nullptr;
-        SDP_TRY(ops_order(ctx, s));
     }
     HIP_TRY(sdpops::launch_qk(a, bf16, backward, s));
     if (sums) SDP_TRY(ops_mark(ctx, s));
@@ -262,12 +268,10 @@ int check_grids(const char *call, const sdpops::GroupedArgs &a, bool forward, bo
 }
 
 // The products of a call, with the workspace that they need.
-int run_grouped(sdp_ctx *ctx, const sdpops::GroupedArgs &a, bool forward, bool dx, bool dw, hipStream_t s) {
+int run_grouped(sdp_ctx *ctx, const char *call, const sdpops::GroupedArgs &a, bool forward, bool dx, bool dw,
+                hipStream_t s) {
     const size_t bytes = sdpops::grouped_workspace(a, forward, dx, dw);
-    if (bytes > 0) {
-        SDP_TRY(ensure_ops_space(ctx, bytes));
-        SDP_TRY(ops_order(ctx, s));
-    }
+    if (bytes > 0) SDP_TRY(take_ops_space(ctx, call, bytes, s));
     HIP_TRY(sdpops::launch_grouped(a, forward, dx, dw, ctx->ops_space, s));
     if (bytes > 0) SDP_TRY(ops_mark(ctx, s));
     return SDP_OK;
@@ -349,9 +353,8 @@ int distill_call(sdp_ctx *ctx, const char *call, const sdp_distill_desc *d, floa
     a.splits = sdpops::distill_splits(a, bf16);
     const bool parts = a.splits > 0 && rows > 0;
     if (parts) {
-        SDP_TRY(ensure_ops_space(ctx, (size_t)rows * a.splits * sdpops::kDistillPartials * sizeof(float)));
+        SDP_TRY(take_ops_space(ctx, call, (size_t)rows * a.splits * sdpops::kDistillPartials * sizeof(float), s));
         a.partials = (float *)ctx->ops_space;
-        SDP_TRY(ops_order(ctx, s));
     }
     HIP_TRY(sdpops::launch_distill(a, bf16, s));
     if (parts) SDP_TRY(ops_mark(ctx, s));
@@ -413,7 +416,7 @@ int sdp_grouped_matmul(sdp_ctx *ctx, const sdp_grouped_desc *desc, const uint16_
                                dense("ends", desc->ends, desc->groups, type_size(desc->ends_type), false),
                                rows_of("y", y, desc->rows, desc->y_stride, out, type_size(desc->out_type), true)},
                               {}));
-        return run_grouped(ctx, a, true, false, false, (hipStream_t)stream);
+        return run_grouped(ctx, call, a, true, false, false, (hipStream_t)stream);
     });
 }
 
@@ -442,7 +445,7 @@ int sdp_grouped_matmul_backward(sdp_ctx *ctx, const sdp_grouped_desc *desc, cons
             ts.push_back(dense("dw", dw, desc->groups * out * in, type_size(desc->out_type), true));
         }
         SDP_TRY(check_tensors(ctx, call, ts, {}));
-        return run_grouped(ctx, a, false, dx != nullptr, dw != nullptr, (hipStream_t)stream);
+        return run_grouped(ctx, call, a, false, dx != nullptr, dw != nullptr, (hipStream_t)stream);
     });
 }
 
