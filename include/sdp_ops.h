@@ -195,7 +195,11 @@ SDP_API int sdp_distill_loss(sdp_ctx *ctx, const sdp_distill_desc *desc, float *
 
 /* The gradient alone, from lse as sdp_distill_loss wrote it:
  *   d loss / d z_v = distill_weight tau (exp(z_v / tau - L_tau) - q_v)
- *                  + label_weight (exp(z_v - L_1) - [v = label]) */
+ *                  + label_weight (exp(z_v - L_1) - [v = label])
+ * L's rounding to FP32, up to 2^-24 |L|, is a relative error of the
+ * exponentials: small for logits around zero, but a row of the type's lowest
+ * value has no L that this can be made from.  The loss and the gradient of
+ * sdp_distill_loss come from the logits' differences and have no such limit. */
 SDP_API int sdp_distill_loss_backward(sdp_ctx *ctx, const sdp_distill_desc *desc, const float *lse,
                                       const float *row_grad, void *dlogits, int64_t dlogits_stride, void *stream);
 

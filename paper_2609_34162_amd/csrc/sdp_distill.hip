@@ -110,13 +110,11 @@ __device__ __forceinline__ Sums wave_join(Sums s, float c_tau) {
     return s;
 }
 
-// L = log of a sum against top, and 1 / sum.
-__device__ __forceinline__ float log_of(float sum, float top, float scale) { return logf(sum) + against(top) * scale; }
-
 // ---- the teacher and the label of a row --------------------------------------------
 
 struct Row {
-    float log_sum;     // of the teacher's exp(t / tau)
+    float t_ref;       // the teacher's largest t, and
+    float log_sum;     // the logarithm of its sum of exp((t - t_ref) / tau)
     bool has_teacher, has_label, bad;
     int32_t label;     // -1: none
 };
@@ -128,17 +126,18 @@ __device__ Row row_of(const DistillArgs &a, int64_t row) {
     for (int j = lane; j < K; j += 64) {
         const int64_t idx = load_int(a.teacher_index, row * K + j, a.index64);
         if (idx >= a.vocab) bad = 1.0f;
-        if (idx >= 0) top = fmaxf(top, load_either(a.teacher_logits, row * K + j, a.teacher_bf16) * a.inv_tau);
+        if (idx >= 0) top = fmaxf(top, load_either(a.teacher_logits, row * K + j, a.teacher_bf16));
     }
     top = wave_max(top);
+    Row r;
+    r.t_ref = against(top);
+    const float c_tau = a.inv_tau * kLog2e;
     float sum = 0.0f;
     for (int j = lane; j < K; j += 64)
         if (load_int(a.teacher_index, row * K + j, a.index64) >= 0)
-            sum += exp2_of((load_either(a.teacher_logits, row * K + j, a.teacher_bf16) * a.inv_tau - against(top)) *
-                           kLog2e);
+            sum += exp2_of((load_either(a.teacher_logits, row * K + j, a.teacher_bf16) - r.t_ref) * c_tau);
     sum = wave_sum(sum);
-    Row r;
-    r.log_sum = logf(sum) + against(top);
+    r.log_sum = logf(sum);
     // a NaN among the teacher's logits leaves top alone and makes the sum NaN
     r.has_teacher = a.distill_weight != 0.0f && (top != kNegInf || sum != 0.0f);
     int64_t label = a.labels && a.label_weight != 0.0f ? load_int(a.labels, row, a.index64) : -1;
@@ -149,43 +148,48 @@ __device__ Row row_of(const DistillArgs &a, int64_t row) {
     return r;
 }
 
-// Entry j: its place in the row (-1: not there, or past the vocabulary), q and log q.
+// Entry j: its place in the row (-1: not there, or past the vocabulary), q and tau log q.
 __device__ __forceinline__ int32_t entry(const DistillArgs &a, int64_t row, const Row &r, int j, float *q,
-                                         float *log_q) {
+                                         float *tau_log_q) {
     const int64_t idx = load_int(a.teacher_index, row * a.k + j, a.index64);
-    *log_q = load_either(a.teacher_logits, row * a.k + j, a.teacher_bf16) * a.inv_tau - r.log_sum;
-    *q = idx >= 0 ? exp2_of(*log_q * kLog2e) : 0.0f;
+    const float t = load_either(a.teacher_logits, row * a.k + j, a.teacher_bf16) - r.t_ref;
+    *tau_log_q = t - a.tau * r.log_sum;
+    *q = idx >= 0 ? exp2_of((t * a.inv_tau - r.log_sum) * kLog2e) : 0.0f;
     return idx >= 0 && idx < a.vocab ? (int32_t)idx : -1;
 }
 
-// What one part of a row says to its loss: sum of q (log q - z / tau) and of q
-// over the entries in [v0, v1), and the label's logit.
+// What one part of a row says to its loss: sum of q (tau log q - (z - ref)) and of q
+// over the entries in [v0, v1), and the label's logit less ref.  A loss comes from
+// differences to the row's largest logit alone: L - z would lose what the logits'
+// distance from zero leaves no bits for, and a row of the type's lowest value has no L.
 struct Terms {
     float dot, q, z_label;
 };
 
 template <typename T>
-__device__ Terms wave_terms(const DistillArgs &a, int64_t row, const Row &r, const T *z, int64_t v0, int64_t v1) {
+__device__ Terms wave_terms(const DistillArgs &a, int64_t row, const Row &r, const T *z, int64_t v0, int64_t v1,
+                            float ref) {
     const int lane = threadIdx.x & 63;
     Terms t{0.0f, 0.0f, 0.0f};
     if (r.has_teacher)
         for (int j = lane; j < a.k; j += 64) {
-            float q, log_q;
-            const int32_t v = entry(a, row, r, j, &q, &log_q);
+            float q, tau_log_q;
+            const int32_t v = entry(a, row, r, j, &q, &tau_log_q);
             if (v < v0 || v >= v1 || q == 0.0f) continue;
-            t.dot += q * (log_q - load1(z + v) * a.inv_tau);
+            t.dot += q * (tau_log_q - (load1(z + v) - ref));
             t.q += q;
         }
     t.dot = wave_sum(t.dot);
     t.q = wave_sum(t.q);
-    if (r.label >= v0 && r.label < v1) t.z_label = load1(z + r.label);
+    if (r.label >= v0 && r.label < v1) t.z_label = load1(z + r.label) - ref;
     return t;
 }
 
-__device__ float loss_of(const DistillArgs &a, const Row &r, const Terms &t, float l_tau, float l_one) {
+// log_tau, log_one: of the sums against the row's largest logit, as the terms are.
+__device__ float loss_of(const DistillArgs &a, const Row &r, const Terms &t, float log_tau, float log_one) {
     float loss = 0.0f;
-    if (r.has_teacher) loss = a.distill_weight * a.tau * a.tau * (t.dot + t.q * l_tau);
-    if (r.has_label) loss += a.label_weight * (l_one - t.z_label);
+    if (r.has_teacher) loss = a.distill_weight * a.tau * (t.dot + t.q * (a.tau * log_tau));
+    if (r.has_label) loss += a.label_weight * (log_one - t.z_label);
     return r.bad ? __builtin_nanf("") : loss;
 }
 
@@ -245,9 +249,9 @@ template <typename T>
 __device__ void gather_entries(const DistillArgs &a, int64_t row, const Row &r, const T *z, int64_t v0, int64_t v1,
                                Entries &e) {
     for (int j = threadIdx.x & 63; j <= a.k; j += 64) {
-        float q = 0.0f, log_q;
+        float q = 0.0f, tau_log_q;
         int32_t v = r.label;
-        if (j < a.k) v = r.has_teacher ? entry(a, row, r, j, &q, &log_q) : -1;
+        if (j < a.k) v = r.has_teacher ? entry(a, row, r, j, &q, &tau_log_q) : -1;
         if (v < v0 || v >= v1) v = -1;
         e.index[j] = v;
         e.q[j] = q;
@@ -354,34 +358,45 @@ __global__ __launch_bounds__(kSplitThreads) void k_distill_sums(DistillArgs a) {
 #pragma unroll
     for (int w = 1; w < kSplitThreads / 64; ++w) s = join(s, waves[w], c_tau);
     Terms t{0.0f, 0.0f, 0.0f};
-    if (a.dlogits) t = wave_terms<T>(a, row, row_of(a, row), z, p.v0, p.v1);
+    bool label_here = false;
+    if (a.dlogits) {
+        const Row r = row_of(a, row);
+        t = wave_terms<T>(a, row, r, z, p.v0, p.v1, against(s.top));
+        label_here = r.label >= p.v0 && r.label < p.v1;
+    }
     if (tid == 0) {
         float *out = a.partials + (row * a.splits + blockIdx.y) * kDistillPartials;
         out[0] = s.top, out[1] = s.tau, out[2] = s.one;
-        out[3] = t.dot, out[4] = t.q, out[5] = t.z_label;
+        out[3] = t.dot, out[4] = t.q, out[5] = t.z_label, out[6] = label_here ? 1.0f : 0.0f;
     }
 }
 
-// The parts of a row joined, by one whole wave.
+// The parts of a row joined, by one whole wave, a lane to each part (parts_of: 64 at most).
 __device__ void join_parts(const DistillArgs &a, int64_t row, Sums *s, Terms *t) {
-    const float c_tau = a.inv_tau * kLog2e;
-    *s = Sums{kNegInf, 0.0f, 0.0f};
+    const int part = threadIdx.x & 63;
+    Sums mine{kNegInf, 0.0f, 0.0f};
     *t = Terms{0.0f, 0.0f, 0.0f};
-    for (int i = threadIdx.x & 63; i < a.splits; i += 64) {
-        const float *p = a.partials + (row * a.splits + i) * kDistillPartials;
-        *s = join(*s, {p[0], p[1], p[2]}, c_tau);
-        t->dot += p[3], t->q += p[4], t->z_label += p[5];
+    bool label_here = false;
+    if (part < a.splits) {
+        const float *p = a.partials + (row * a.splits + part) * kDistillPartials;
+        mine = Sums{p[0], p[1], p[2]};
+        *t = Terms{p[3], p[4], p[5]};
+        label_here = p[6] != 0.0f;
     }
-    *s = wave_join(*s, c_tau);
+    *s = wave_join(mine, a.inv_tau * kLog2e);
+    // the terms from the part's largest logit to the row's
+    const float up = against(mine.top) - against(s->top);
+    if (t->q != 0.0f) t->dot -= t->q * up;
+    if (label_here) t->z_label += up;
     t->dot = wave_sum(t->dot), t->q = wave_sum(t->q), t->z_label = wave_sum(t->z_label);
 }
 
 __device__ void write_loss(const DistillArgs &a, int64_t row, const Row &r, const Sums &s, const Terms &t) {
-    const float l_tau = log_of(s.tau, s.top, a.inv_tau), l_one = log_of(s.one, s.top, 1.0f);
-    a.loss[row] = loss_of(a, r, t, l_tau, l_one);
+    const float log_tau = logf(s.tau), log_one = logf(s.one), ref = against(s.top);
+    a.loss[row] = loss_of(a, r, t, log_tau, log_one);
     if (a.lse) {
-        a.lse[2 * row] = l_tau;
-        a.lse[2 * row + 1] = l_one;
+        a.lse[2 * row] = log_tau + ref * a.inv_tau;
+        a.lse[2 * row + 1] = log_one + ref;
     }
 }
 
@@ -393,7 +408,7 @@ __global__ __launch_bounds__(64) void k_distill_loss(DistillArgs a) {
     Sums s;
     Terms t;
     join_parts(a, row, &s, &t);
-    t = wave_terms<T>(a, row, r, (const T *)a.logits + row * a.logit_stride, 0, a.vocab);
+    t = wave_terms<T>(a, row, r, (const T *)a.logits + row * a.logit_stride, 0, a.vocab, against(s.top));
     if (threadIdx.x == 0) write_loss(a, row, r, s, t);
 }
 
@@ -478,7 +493,7 @@ __device__ __forceinline__ float top_of_bits(s16x8 m) {
 template <typename T, int THREADS, int NV, int SUMS, int POWER>
 __global__ __launch_bounds__(THREADS) void k_distill_resident(DistillArgs a) {
     constexpr int kN = kPer<T>, kWaves = THREADS / 64;
-    // the entries (q: t / tau at first, then q times t_sum) of this row and the next;
+    // the entries (q: t at first, then q times t_sum) of this row and the next;
     // entry j, and the label as entry k, belong to thread j mod THREADS
     __shared__ Entries both[2];
     __shared__ float red[4][kWaves];
@@ -493,7 +508,7 @@ __global__ __launch_bounds__(THREADS) void k_distill_resident(DistillArgs a) {
     int64_t row = blockIdx.x;
     // a thread's pieces are THREADS apart: one offset, and a scalar base for each
     const uint32_t at = (uint32_t)tid * kN;
-    // places and t / tau of a row's entries (-inf where their term is off); an index past
+    // places and t of a row's entries (-inf where their term is off); an index past
     // the vocabulary is kept as its size
     auto fetch_entries = [&](int64_t of, Entries &en) __attribute__((always_inline)) {
 #pragma unroll 1
@@ -502,7 +517,7 @@ __global__ __launch_bounds__(THREADS) void k_distill_resident(DistillArgs a) {
             float t = kNegInf;
             if (j < a.k) {
                 v = load_int(a.teacher_index, of * a.k + j, a.index64);
-                if (teacher) t = load_either(a.teacher_logits, of * a.k + j, a.teacher_bf16) * a.inv_tau;
+                if (teacher) t = load_either(a.teacher_logits, of * a.k + j, a.teacher_bf16);
             } else if (labels) {
                 v = load_int(a.labels, of, a.index64);
             }
@@ -579,14 +594,14 @@ __global__ __launch_bounds__(THREADS) void k_distill_resident(DistillArgs a) {
             top = block_top(top, t_top, &t_top);
         }
         const float ref = against(top), t_ref = against(t_top);
-        // the teacher's sum of exp(t / tau - top), and of that times t / tau - top - z / tau
+        // the teacher's sum of exp((t - t_ref) / tau), and of that times t - t_ref - (z - ref)
         float t_sum = 0.0f, t_dot = 0.0f;
 #pragma unroll 1
         for (int j = tid; j <= a.k; j += THREADS) {
             const float t = entries.q[j];
-            const float q = t != kNegInf ? exp2_of((t - t_ref) * kLog2e) : 0.0f;
+            const float q = t != kNegInf ? exp2_of((t - t_ref) * c_tau) : 0.0f;
             t_sum += q;
-            if (q != 0.0f) t_dot += q * (t - t_ref - entries.z[j] * a.inv_tau);
+            if (q != 0.0f) t_dot += q * (t - t_ref - (entries.z[j] - ref));
             entries.q[j] = q;
             if (entries.index[j] == a.vocab) entries.index[j] = -1;
         }
@@ -613,8 +628,8 @@ __global__ __launch_bounds__(THREADS) void k_distill_resident(DistillArgs a) {
         r.label = labels ? entries.index[a.k] : -1;
         r.has_label = r.label >= 0;
         if (tid == 0) {
-            // sum of q (log q - z / tau), the q's sum being 1
-            Terms terms{t_dot / t_sum - logf(t_sum), 1.0f, entries.z[a.k]};
+            // sum of q (tau log q - (z - ref)), the q's sum being 1
+            Terms terms{t_dot / t_sum - a.tau * logf(t_sum), 1.0f, entries.z[a.k] - ref};
             write_loss(a, row, r, s, terms);
         }
         Slope d = slope_of<POWER, false>(a, r, a.row_grad[row], s, 0.0f, 0.0f);
