@@ -268,7 +268,8 @@ __device__ void correct_entries(const DistillArgs &a, const Row &r, const Slope 
         if (v < 0) continue;
         float q = 0.0f;
         for (int i = 0; i < a.k; ++i) q += e.index[i] == v ? e.q[i] : 0.0f;
-        float s = slope_at<POWER, BACK>(d, e.z[j]) - d.g_tau * q;
+        float s = slope_at<POWER, BACK>(d, e.z[j]);
+        if (q != 0.0f) s -= d.g_tau * q;  // (a NaN in the teacher's sum is not the label's)
         if (v == r.label) s -= d.g_one;
         store1(dz + v, s);
     }

@@ -111,3 +111,74 @@ def test_a_weight_of_zero_leaves_the_teacher_out(ctx, rows, dtype, value):
         got.append(out)
     for a, b in zip(*got):
         assert torch.isfinite(a).all() and torch.equal(bits(a), bits(b))
+
+
+# rows of 8 to 19 pieces to each of 1,024 threads (and of 16 to each of 256), with and without a short last piece
+LARGE = [(BF16, 30005), (BF16, 40000), (BF16, 65536), (BF16, 90003), (BF16, 120011), (BF16, 151936), (BF16, 155655),
+         (F32, 16001), (F32, 20003), (F32, 45001), (F32, 60007), (F32, 77827)]
+
+
+@pytest.mark.parametrize("tau", [1.0, 2.0, 3.0, 4.0, 1.5])
+@pytest.mark.parametrize("dtype,vocab", LARGE)
+def test_long_rows(ctx, dtype, vocab, tau):
+    check_some(ctx, make(vocab, 40, dtype, seed=vocab), tau)
+
+
+@pytest.mark.parametrize("a,b,labels", [(1.0, 0.0, True), (0.0, 1.0, True), (0.7, 0.0, False)])
+@pytest.mark.parametrize("dtype,vocab", [(BF16, 3000), (BF16, 90003), (F32, 45001)])
+def test_one_term_alone(ctx, dtype, vocab, a, b, labels):
+    check_some(ctx, make(vocab, 12, dtype, labels=labels, seed=7), 3.0, a, b)
+
+
+def planted(st, dtype):
+    """Masked logits, absent and masked entries, indexes named twice, rows with nothing, in the first ten rows."""
+    z, index, teacher, labels = st["z"], st["index"], st["teacher"], st["labels"]
+    vocab, eight = z.shape[1], torch.arange(8, device="cuda")
+    z[0, vocab // 2:] = -INF
+    z[1, : vocab - 5] = torch.finfo(dtype).min
+    index[0], labels[0] = eight, 1
+    index[1], labels[1] = torch.arange(vocab - 8, vocab, device="cuda"), vocab - 1
+    teacher[1, :3] = -INF
+    index[2], labels[2] = -1, 3
+    index[3], labels[3] = -1, -100
+    teacher[4, 2:], index[4] = -INF, eight
+    teacher[5], index[5], labels[5] = -INF, eight, -1
+    teacher[6, 1:], index[6] = torch.finfo(F32).min, eight
+    z[7, :] = -INF
+    z[7, 17] = 2.0
+    index[7], labels[7] = -1, 17
+    index[8, :4] = 9
+    z[9] = -z[9].abs() - 1.0  # nothing but negative values
+    st["row_grad"][[4, 77, 256]] = torch.tensor([-2.0, 0.0, 0.0], device="cuda")
+    return st
+
+
+@pytest.mark.parametrize("tau", [1.0, 2.0, 3.0, 4.0])
+@pytest.mark.parametrize("dtype,vocab", [(BF16, 500), (BF16, 2053), (BF16, 20000), (BF16, 90003), (F32, 501),
+                                         (F32, 20003), (F32, 60007)])
+def test_masks(ctx, dtype, vocab, tau):
+    check_some(ctx, planted(make(vocab, 8, dtype, seed=2), dtype), tau)
+
+
+@pytest.mark.parametrize("dtype,vocab", [(BF16, 2053), (BF16, 90003), (F32, 20003)])
+def test_values_out_of_range_and_nan_reach_their_rows_only(ctx, dtype, vocab):
+    from paper_2609_34162_amd import ops
+    st = make(vocab, 4, dtype, seed=5)
+    z, index, labels = st["z"], st["index"], st["labels"]
+    index[:] = torch.arange(4, device="cuda")
+    labels[:] = 5
+    index[1, 2], index[2, 0], labels[3] = vocab, 1 << 40, vocab
+    check_some(ctx, st)
+    z[6, vocab // 3], z[256, vocab - 1], st["teacher"][7, 1] = float("nan"), -float("nan"), float("nan")
+    z[8], index[8], labels[8] = float("nan"), -1, -100  # learned from by nobody
+    loss, d = torch.full((ROWS,), 7.0, device="cuda"), torch.full_like(z, 7.0)
+    ops.sdp_distill_loss(ctx, z, loss, None, teacher_logits=st["teacher"], teacher_index=index, labels=labels,
+                         label_weight=0.5, row_grad=st["row_grad"], dlogits=d)
+    lost = torch.zeros(ROWS, dtype=torch.bool, device="cuda")
+    lost[[1, 2, 3, 6, 256, 7]] = True
+    assert torch.equal(loss.isnan(), lost) and torch.isfinite(loss[~lost]).all()
+    whole = lost.clone()
+    whole[7] = False  # the entries alone
+    assert torch.equal(d.isnan().all(1), whole) and torch.isfinite(d[~lost]).all()
+    assert d[7, :4].isnan().all() and torch.isfinite(d[7, 4:]).all()
+    assert loss[8] == 0 and not d[8].any()
