@@ -75,26 +75,44 @@ inline bool same_tensor(const char *pa, const Layout &a, const char *pb, const L
     return true;
 }
 
+// The outer dimensions (0 and 1) of two tensors that step alike there, around `inner`
+// elements of each step: of a buffer that holds both.
+inline Layout around(const Layout &a, const Layout &b, int64_t inner) {
+    Layout all{{1, 1, 1}, {0, 0, 0}, inner};
+    for (int k = 0; k < 2; ++k) {
+        all.ext[k] = a.ext[k] > b.ext[k] ? a.ext[k] : b.ext[k];
+        all.stride[k] = a.ext[k] > 1 ? a.stride[k] : b.stride[k];
+    }
+    return all;
+}
+
+// Whether `hi`, which starts `apart` elements past `lo`, lies in other columns of the
+// same rows: past all that lo has of a row, and before its next one.
+inline bool other_columns(const Layout &lo, const Layout &hi, int64_t apart) {
+    for (int k = 0; k < 2; ++k)
+        if (lo.ext[k] > 1 && hi.ext[k] > 1 && lo.stride[k] != hi.stride[k]) return false;
+    const int64_t lo_width = (lo.ext[2] - 1) * lo.stride[2] + lo.inner, hi_width = (hi.ext[2] - 1) * hi.stride[2] + hi.inner;
+    return apart >= lo_width && injective(around(lo, hi, apart + hi_width));
+}
+
 // Whether two tensors of elements of `size` bytes share no element: their
-// byte ranges are apart, or they are runs of heads (dimension 2) of one fused
-// tensor, whose runs do not meet.  Where neither can be shown, false.
+// byte ranges are apart, or they are columns of the same rows, or runs of heads
+// (dimension 2) of one fused tensor, whose runs do not meet.  Where none can be
+// shown, false.
 inline bool disjoint(const char *pa, const Layout &a, const char *pb, const Layout &b, int64_t size) {
     if (no_elements(a) || no_elements(b)) return true;
     const int64_t sa = span(a) * size, sb = span(b) * size;
     if (pa + sa <= pb || pb + sb <= pa) return true;
-    if (a.inner != b.inner || !same_strides(a, b)) return false;
     const bool a_first = pa <= pb;
     const Layout &lo = a_first ? a : b, &hi = a_first ? b : a;
     const int64_t apart = a_first ? pb - pa : pa - pb;
+    if (apart % size == 0 && other_columns(lo, hi, apart / size)) return true;
+    if (a.inner != b.inner || !same_strides(a, b)) return false;
     const int64_t hs = lo.ext[2] > 1 ? lo.stride[2] : hi.ext[2] > 1 ? hi.stride[2] : lo.inner;
     if (hs < lo.inner || apart % (hs * size) != 0) return false;
     const int64_t first = apart / (hs * size);
     if (first < lo.ext[2]) return false;
-    Layout all = lo;
-    for (int k = 0; k < 2; ++k) {
-        if (lo.ext[k] <= 1) all.stride[k] = hi.stride[k];
-        if (hi.ext[k] > all.ext[k]) all.ext[k] = hi.ext[k];
-    }
+    Layout all = around(lo, hi, lo.inner);
     all.stride[2] = hs;
     all.ext[2] = first + hi.ext[2];
     return injective(all);
