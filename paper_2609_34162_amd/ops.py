@@ -181,8 +181,9 @@ def _qk_desc(q, k, cos, sin, q_weight, k_weight, positions, eps, interleaved):
     at, position_type = None, SDP_TYPE_I32
     if positions is not None:
         position_type = _type(positions, "positions")
-        _want(positions.numel() == batch * tokens and positions.is_contiguous(),
-              "positions must be [batch, tokens], contiguous")
+        given = positions.shape
+        if given != (batch, tokens) and given != (batch * tokens,) or not positions.is_contiguous():
+            raise ValueError(f"positions must be [{batch}, {tokens}] (or in one dimension), contiguous")
         at = positions.data_ptr()
     # in the fields' order: several times as fast as setting them one by one
     d = sdp_qk_norm_rope_desc(code, weight_type, batch, tokens, q_heads, k_heads, dim, rotary, 1 if interleaved else 0,
