@@ -207,7 +207,7 @@ struct Slope {
 template <int POWER, bool BACK>
 __device__ Slope slope_of(const DistillArgs &a, const Row &r, float g, Sums sums, float l_tau, float l_one) {
     Slope d;
-    g = r.bad ? __builtin_nanf("") : g;
+    g = r.bad && g != 0.0f ? __builtin_nanf("") : g;
     d.g_tau = r.has_teacher || r.bad ? g * a.distill_weight * a.tau : 0.0f;
     d.g_one = r.has_label || r.bad ? g * a.label_weight : 0.0f;
     const float ref = against(sums.top);

@@ -182,3 +182,21 @@ def test_values_out_of_range_and_nan_reach_their_rows_only(ctx, dtype, vocab):
     assert torch.equal(d.isnan().all(1), whole) and torch.isfinite(d[~lost]).all()
     assert d[7, :4].isnan().all() and torch.isfinite(d[7, 4:]).all()
     assert loss[8] == 0 and not d[8].any()
+
+
+@pytest.mark.parametrize("rows", [8, ROWS])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_row_grad_of_zero_makes_a_zero_gradient(ctx, rows, dtype):
+    """Also of rows whose logits are NaN, or whose entries or label are out of range (their losses are NaN)."""
+    st = make(2003, 4, dtype, rows=rows, seed=9)
+    st["index"][:], st["labels"][:] = torch.arange(4, device="cuda"), 5
+    st["index"][1, 2], st["labels"][2] = 2003, 2003
+    st["row_grad"][:4] = 0.0
+    st["index"][4, 0] = 1 << 40  # this one's gradient is NaN
+    check_some(ctx, st, 2.0, some=[r for r in SOME if r < rows])
+    from paper_2609_34162_amd import ops
+    st["z"][3] = float("nan")
+    loss, d = torch.empty(rows, device="cuda"), torch.full_like(st["z"], 7.0)
+    ops.sdp_distill_loss(ctx, st["z"], loss, None, teacher_logits=st["teacher"], teacher_index=st["index"],
+                         labels=st["labels"], label_weight=0.5, row_grad=st["row_grad"], dlogits=d)
+    assert loss[1:5].isnan().all() and not d[:4].any() and d[4].isnan().all() and torch.isfinite(d[5:]).all()
