@@ -53,3 +53,19 @@ def test_sums_over_as_many_rows_as_32_bits_count(lib, n):
     ops.sdp_grouped_matmul_backward(ctx, x, w, torch.tensor([rows], device="cuda"), dy, None, dw)
     want = -float(rows) * (2.0 ** (power[None, :] - power[:, None]).double())
     assert ((dw[0].double() - want).abs() <= 64 * 2.0 ** -24 * want.abs()).all(), dw
+
+
+@pytest.mark.parametrize("rows,n,groups", [(5, 24, 2), (5, 7, 3), (70001, 1024, 2), (3000, 1021, 0)])
+@pytest.mark.parametrize("out", [BF16, F32])
+def test_empty_contractions_write_zeros(lib, rows, n, groups, out):
+    """y of no inputs, dx of no outputs and dw of no rows, in tiles of every kind."""
+    sdp, ops, ctx = lib
+    ends = torch.tensor([rows // 3, rows][:groups], dtype=torch.int64, device="cuda") if groups < 3 else \
+        torch.tensor([1, 1, rows], device="cuda")
+    e = lambda *shape: torch.empty(shape, dtype=BF16, device="cuda")
+    y, dx = torch.full((rows, n), 7.0, dtype=out, device="cuda"), torch.full((rows, n), 7.0, dtype=BF16, device="cuda")
+    ops.sdp_grouped_matmul(ctx, e(rows, 0), e(groups, n, 0), ends, y)
+    ops.sdp_grouped_matmul_backward(ctx, None, e(groups, 0, n), ends, e(rows, 0), dx, None)
+    dw = torch.full((groups, n, n), 7.0, dtype=out, device="cuda")
+    ops.sdp_grouped_matmul_backward(ctx, e(0, n), e(groups, n, n), ends.zero_(), e(0, n), e(0, n), dw)
+    assert not y.any() and not dx.any() and not dw.any()
