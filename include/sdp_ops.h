@@ -23,9 +23,9 @@
  *  - An output may overlap an input or another output only where a call says
  *    so; other overlaps are refused.
  *  - Every call is asynchronous on `stream`.  Calls that use the context's
- *    workspace (sdp_qk_norm_rope_backward with weight gradients, the
- *    distillation loss where a row is split over blocks, gradients of
- *    few experts' weights, grouped products of sizes or strides without whole
+ *    workspace (sdp_qk_norm_rope_backward with weight gradients,
+ *    sdp_distill_loss except where rows stay in registers, gradients of few
+ *    experts' weights, large grouped products of sizes or strides without whole
  *    16-byte pieces) order themselves after the context's last such call, whatever
  *    its stream; a workspace that has to grow waits for the device.  It stays as
  *    large as its largest call needed until the context is destroyed.
