@@ -1,38 +1,16 @@
 // C ABI of libsdp, the training operators (include/sdp_ops.h): checks of the
 // arguments, the context's workspace for them, and the launches.  The kernels
 // are in sdp_qk.hip, sdp_grouped.hip and sdp_distill.hip.
+#include "sdp_ops_host.h"
 #include "sdp_ops_internal.h"
-#include "sdp_ops_plan.h"
-#include "sdp_rt.h"
 
 using namespace sdprt;
-using sdpops::Layout;
 
-namespace {
+namespace sdpops {
 
 // ---- checks -----------------------------------------------------------------
 
-bool is_float_type(int t) { return t == SDP_TYPE_F32 || t == SDP_TYPE_BF16; }
-bool is_int_type(int t) { return t == SDP_TYPE_I32 || t == SDP_TYPE_I64; }
-int64_t type_size(int t) { return t == SDP_TYPE_BF16 ? 2 : t == SDP_TYPE_I64 ? 8 : 4; }
-
-// A buffer of a call: where it lies, and whether the call writes it.
-struct Tensor {
-    const char *what;
-    const void *p;
-    Layout layout;
-    int64_t size;  // of an element
-    bool written;
-};
-
-Tensor dense(const char *what, const void *p, int64_t n, int64_t size, bool written) {
-    return {what, p, Layout{{1, 1, 1}, {0, 0, 0}, n}, size, written};
-}
-Tensor rows_of(const char *what, const void *p, int64_t rows, int64_t stride, int64_t cols, int64_t size, bool written) {
-    return {what, p, Layout{{1, rows, 1}, {0, rows > 1 ? stride : 0, 0}, cols}, size, written};
-}
-
-int check_memory(const sdp_ctx *ctx, const char *call, const Tensor &t, int64_t bytes) {
+static int check_memory(const sdp_ctx *ctx, const char *call, const Tensor &t, int64_t bytes) {
     hipPointerAttribute_t at;
     if (hipPointerGetAttributes(&at, t.p) != hipSuccess) {
         (void)hipGetLastError();
@@ -53,9 +31,6 @@ int check_memory(const sdp_ctx *ctx, const char *call, const Tensor &t, int64_t 
     return SDP_OK;
 }
 
-// Every buffer lies in device memory of the context's GPU, aligned to its
-// elements; no output overlaps itself or another buffer, except that a pair of
-// in_place (indexes into ts) may be the very same tensor.
 int check_tensors(const sdp_ctx *ctx, const char *call, const std::vector<Tensor> &ts,
                   const std::vector<std::pair<int, int>> &in_place) {
     for (const Tensor &t : ts) {
@@ -96,7 +71,7 @@ int check_tensors(const sdp_ctx *ctx, const char *call, const std::vector<Tensor
 
 // ---- workspace ----------------------------------------------------------------
 
-int ensure_ops_space(sdp_ctx *ctx, size_t bytes) {
+static int ensure_ops_space(sdp_ctx *ctx, size_t bytes) {
     if (bytes <= ctx->ops_space_cap) return SDP_OK;
     HIP_TRY(hipDeviceSynchronize());
     if (ctx->ops_space) HIP_TRY(hipFree(ctx->ops_space));
@@ -112,9 +87,6 @@ int ensure_ops_space(sdp_ctx *ctx, size_t bytes) {
     return SDP_OK;
 }
 
-// The workspace for a call, which then runs after the last one that used it.  A
-// captured graph would keep the workspace's address after it has grown, and the
-// context's event would become part of the capture, so such a call is refused.
 int take_ops_space(sdp_ctx *ctx, const char *call, size_t bytes, hipStream_t s) {
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
     if (s) HIP_TRY(hipStreamIsCapturing(s, &capture));
@@ -129,6 +101,12 @@ int ops_mark(sdp_ctx *ctx, hipStream_t s) {
     ctx->ops_done_valid = true;
     return SDP_OK;
 }
+
+}  // namespace sdpops
+
+using namespace sdpops;
+
+namespace {
 
 // ---- norms of queries and keys -------------------------------------------------
 
@@ -359,20 +337,6 @@ int distill_call(sdp_ctx *ctx, const char *call, const sdp_distill_desc *d, floa
     HIP_TRY(sdpops::launch_distill(a, bf16, s));
     if (parts) SDP_TRY(ops_mark(ctx, s));
     return SDP_OK;
-}
-
-// No C++ exception leaves a C entry point: what allocates here is the host's
-// own bookkeeping.
-template <class F>
-int guarded(F &&body) {
-    t_err.clear();
-    try {
-        return body();
-    } catch (const std::bad_alloc &) {
-        return fail(SDP_ERR_OUT_OF_MEMORY, "out of host memory");
-    } catch (const std::exception &e) {
-        return fail(SDP_ERR_INVALID_ARGUMENT, "%s", e.what());
-    }
 }
 
 }  // namespace
