@@ -11,7 +11,8 @@ LIB_PATH = os.path.join(HERE, "libsdp.so")
 SOURCES = [os.path.join(HERE, "csrc", f)
            for f in ("sdp_runtime.hip", "sdp_stream.hip", "sdp_host_route.hip", "sdp_kernels.hip",
                      "sdp_copy.hip", "sdp_noalloc.hip", "sdp_ops.hip", "sdp_qk.hip", "sdp_grouped.hip",
-                     "sdp_distill.hip")]
+                     "sdp_distill.hip", "sdp_layer.hip", "sdp_embed.hip", "sdp_norm.hip", "sdp_route.hip",
+                     "sdp_order.hip", "sdp_experts.hip")]
 # host-only lanes, built with the host compiler: no fused multiply-add, so the
 # FP64 update rounds every product and sum as written
 HOST_SOURCES = [os.path.join(HERE, "csrc", f) for f in ("sdp_host_adamw.cpp", "sdp_schedule.cpp")]

@@ -1,5 +1,5 @@
-"""ctypes binding of the training operators (include/sdp_ops.h): argument
-marshalling only.
+"""ctypes binding of the training operators (include/sdp_ops.h and
+include/sdp_layer.h): argument marshalling only.
 
 Every function here has the name of the C entry point it calls; it takes torch
 tensors, checks that their shapes belong together and passes their addresses
@@ -22,6 +22,13 @@ SDP_QK_MAX_HEADS = 16384
 SDP_DISTILL_MAX_K = 1024
 SDP_DISTILL_MAX_ROWS = 4000000
 SDP_GROUPED_MAX_GROUPS = 2048
+SDP_ROUTE_MAX_EXPERTS = 2048
+SDP_ROUTE_MAX_TOP = 64
+SDP_ROUTE_MAX_GROUPS = 64
+SDP_GATE_NONE = 0
+SDP_GATE_CHANNEL = 1
+SDP_GATE_TOKEN = 2
+SDP_GATE_ELEMENT = 3
 
 
 class sdp_heads(ctypes.Structure):
@@ -50,10 +57,66 @@ class sdp_distill_desc(ctypes.Structure):
                [(n, ctypes.c_double) for n in ("temperature", "distill_weight", "label_weight")]
 
 
+class sdp_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+
+
+class sdp_embed_desc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64)] + \
+               [(n, ctypes.c_int32) for n in ("vocab", "hidden", "table_type", "row_type", "id_type")] + \
+               [("ids", ctypes.c_void_p), ("scale", ctypes.c_double)]
+
+
+class sdp_block_norm_desc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64)] + \
+               [(n, ctypes.c_int32) for n in ("hidden", "stream_type", "type", "weight_type", "post_norm", "gate_form",
+                                              "gate_sigmoid")] + \
+               [(n, ctypes.c_double) for n in ("scale", "eps", "weight_offset")] + \
+               [("gate", ctypes.c_void_p), ("gate_stride", ctypes.c_int64), ("post_weight", ctypes.c_void_p),
+                ("pre_weight", ctypes.c_void_p)]
+
+
+class sdp_block_norm_grads(ctypes.Structure):
+    _fields_ = [("dh", ctypes.POINTER(sdp_rows)), ("dy", ctypes.POINTER(sdp_rows)), ("dgate", ctypes.c_void_p),
+                ("dgate_stride", ctypes.c_int64), ("dpost_weight", ctypes.c_void_p),
+                ("dpre_weight", ctypes.c_void_p)]
+
+
+class sdp_route_desc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64)] + \
+               [(n, ctypes.c_int32) for n in ("experts", "top", "logit_type", "index_type", "weight_type", "sigmoid",
+                                              "renormalize", "groups", "top_groups", "group_best")] + \
+               [("scale", ctypes.c_double), ("logit_stride", ctypes.c_int64)]
+
+
+class sdp_order_desc(ctypes.Structure):
+    _fields_ = [("entries", ctypes.c_int64)] + \
+               [(n, ctypes.c_int32) for n in ("experts", "index_type", "ends_type")]
+
+
+class sdp_expert_desc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64)] + \
+               [(n, ctypes.c_int32) for n in ("top", "hidden", "row_type", "stream_type", "weight_type")] + \
+               [("place", ctypes.c_void_p)]
+
+
 def _bind():
-    vp, i64, P = ctypes.c_void_p, ctypes.c_int64, ctypes.POINTER
+    vp, i32, i64, P = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.POINTER
     h, qk, gm, ds = P(sdp_heads), P(sdp_qk_norm_rope_desc), P(sdp_grouped_desc), P(sdp_distill_desc)
+    r, em, bn, rt, od, ex = (P(t) for t in (sdp_rows, sdp_embed_desc, sdp_block_norm_desc, sdp_route_desc,
+                                            sdp_order_desc, sdp_expert_desc))
     for name, args in {
+        "sdp_embed": [vp, em, r, r, vp],
+        "sdp_embed_backward": [vp, em, r, r, i32, vp],
+        "sdp_block_norm": [vp, bn, r, r, r, r, vp],
+        "sdp_block_norm_backward": [vp, bn, r, r, r, r, P(sdp_block_norm_grads), vp],
+        "sdp_route": [vp, rt, vp, vp, vp, vp, vp],
+        "sdp_route_backward": [vp, rt, vp, vp, vp, vp, i64, vp],
+        "sdp_expert_order": [vp, od, vp, vp, vp, vp, vp],
+        "sdp_expert_gather": [vp, ex, r, r, vp],
+        "sdp_expert_gather_backward": [vp, ex, r, r, vp],
+        "sdp_expert_combine": [vp, ex, r, vp, r, r, vp],
+        "sdp_expert_combine_backward": [vp, ex, r, vp, r, r, vp, vp],
         "sdp_qk_norm_rope": [vp, qk, h, h, h, h, vp],
         "sdp_qk_norm_rope_backward": [vp, qk, h, h, h, h, h, h, vp, vp, vp],
         "sdp_grouped_matmul": [vp, gm, vp, vp, vp, vp],
@@ -316,3 +379,196 @@ def sdp_distill_loss_backward(ctx, logits, lse, row_grad, dlogits, *, teacher_lo
     at, stride = _dlogits(d, shape, dlogits)
     _check(_lib.sdp_distill_loss_backward(ctx, d, _f32(lse, (shape[0], 2), "lse"),
                                           _f32(row_grad, (shape[0],), "row_grad"), at, stride, _stream(stream)))
+
+
+# ---- around the experts' products (include/sdp_layer.h) ------------------------
+
+def _rows(t, shape, code: int, what: str) -> Optional[sdp_rows]:
+    """A 2-D tensor of this shape and type (None passes)."""
+    if t is None:
+        return None
+    _same_type(t, code, what)
+    return sdp_rows(t.data_ptr(), _row_stride(t, shape, what))
+
+
+def _two(t, what: str):
+    shape = t.shape
+    _want(len(shape) == 2, f"{what} must be 2-D")
+    return shape
+
+
+def _embed_desc(table, rows, tokens, scale, names):
+    vocab, hidden = _two(table, names[0])
+    _count(max(vocab, hidden), names[0])
+    shape = tokens.shape
+    _want(len(shape) == 1, "tokens must be 1-D")
+    n = shape[0]
+    table_type, row_type = _type(table, names[0]), _type(rows, names[1])
+    d = sdp_embed_desc(n, vocab, hidden, table_type, row_type, _type(tokens, "tokens"),
+                       _dense(tokens, shape, "tokens"), scale)
+    return d, _rows(table, (vocab, hidden), table_type, names[0]), _rows(rows, (n, hidden), row_type, names[1])
+
+
+def sdp_embed(ctx, table, tokens, out, *, scale: float = 1.0, stream=None) -> None:
+    d, t, o = _embed_desc(table, out, tokens, scale, ("table", "out"))
+    _check(_lib.sdp_embed(ctx, d, t, o, _stream(stream)))
+
+
+def sdp_embed_backward(ctx, dout, tokens, dtable, *, scale: float = 1.0, accumulate: bool = False,
+                       stream=None) -> None:
+    d, t, o = _embed_desc(dtable, dout, tokens, scale, ("dtable", "dout"))
+    _check(_lib.sdp_embed_backward(ctx, d, o, t, 1 if accumulate else 0, _stream(stream)))
+
+
+def _gate(t, tokens: int, hidden: int, code: int, what: str):
+    """Form, address and stride of a gate [hidden] or [1, hidden], [tokens, 1] or
+    [tokens, hidden]; of one token or one channel the form of the most elements."""
+    if t is None:
+        return SDP_GATE_NONE, None, 0
+    _same_type(t, code, what)
+    shape, strides = t.shape, t.stride()
+    if shape == (hidden,) or (shape == (1, hidden) and tokens != 1):
+        return SDP_GATE_CHANNEL, _dense(t, shape, what), 0
+    if shape == (tokens, hidden):
+        return SDP_GATE_ELEMENT, t.data_ptr(), _row_stride(t, shape, what)
+    if shape == (tokens, 1):
+        return SDP_GATE_TOKEN, t.data_ptr(), strides[0]
+    raise ValueError(f"{what} has shape {tuple(shape)}, expected [{hidden}], [{tokens}, 1] or [{tokens}, {hidden}]")
+
+
+def _block_norm_desc(stream_t, y_t, weights, gate, sigmoid, post_norm, post_weight, pre_weight, scale, eps, offset):
+    """stream_t, y_t: any tensor of the stream, and of y's type (None: the gate's, or the stream's)."""
+    shape = _two(stream_t, "the stream")
+    tokens, hidden = shape
+    _count(hidden, "the stream")
+    stream_type = _type(stream_t, "the stream")
+    some = gate if y_t is None else y_t
+    code = stream_type if some is None else _type(some, "y")
+    given = [w for w in weights if w is not None]
+    weight_type = _type(given[0], "a weight") if given else SDP_TYPE_F32
+    for w in given:
+        _same_type(w, weight_type, "a weight")
+    form, at, stride = _gate(gate, tokens, hidden, code, "gate")
+    d = sdp_block_norm_desc(tokens, hidden, stream_type, code, weight_type, 1 if post_norm else 0, form,
+                            1 if sigmoid else 0, scale, eps, offset, at, stride,
+                            _dense(post_weight, (hidden,), "post_weight"), _dense(pre_weight, (hidden,), "pre_weight"))
+    return d, shape
+
+
+def sdp_block_norm(ctx, h, y, h_out, n_out, *, gate=None, gate_sigmoid: bool = False, post_norm: bool = False,
+                   post_weight=None, pre_weight=None, scale: float = 1.0, eps: float = 1e-6,
+                   weight_offset: float = 0.0, stream=None) -> None:
+    """y and h_out may be None (the norm alone), or n_out."""
+    d, shape = _block_norm_desc(h, n_out if y is None else y, (post_weight, pre_weight), gate, gate_sigmoid, post_norm,
+                                post_weight, pre_weight, scale, eps, weight_offset)
+    s, c = d.stream_type, d.type
+    _check(_lib.sdp_block_norm(ctx, d, _rows(h, shape, s, "h"), _rows(y, shape, c, "y"), _rows(h_out, shape, s, "h_out"),
+                               _rows(n_out, shape, c, "n_out"), _stream(stream)))
+
+
+def sdp_block_norm_backward(ctx, h_out, y, dh_out, dn, dh, dy, *, gate=None, dgate=None, gate_sigmoid: bool = False,
+                            post_norm: bool = False, post_weight=None, dpost_weight=None, pre_weight=None,
+                            dpre_weight=None, scale: float = 1.0, eps: float = 1e-6, weight_offset: float = 0.0,
+                            stream=None) -> None:
+    """h_out is the stream after the addition; any tensor that the call does not need may be None."""
+    first = [t for t in (h_out, dh_out, dh) if t is not None]
+    _want(bool(first), "h_out, dh_out and dh are all None")
+    ys = [t for t in (y, dn, dy) if t is not None]
+    d, shape = _block_norm_desc(first[0], ys[0] if ys else None, (post_weight, pre_weight, dpost_weight, dpre_weight),
+                                gate, gate_sigmoid, post_norm, post_weight, pre_weight, scale, eps, weight_offset)
+    s, c = d.stream_type, d.type
+    form, at, stride = _gate(dgate, shape[0], shape[1], c, "dgate")
+    if dgate is not None and form != d.gate_form:
+        raise ValueError("dgate has another form than gate")
+    wide = (shape[1],)
+    rows_dh, rows_dy = _rows(dh, shape, s, "dh"), _rows(dy, shape, c, "dy")
+    ref = lambda r: None if r is None else ctypes.pointer(r)
+    grads = sdp_block_norm_grads(ref(rows_dh), ref(rows_dy), at, stride, _dense(dpost_weight, wide, "dpost_weight"),
+                                 _dense(dpre_weight, wide, "dpre_weight"))
+    _check(_lib.sdp_block_norm_backward(ctx, d, _rows(h_out, shape, s, "h_out"), _rows(y, shape, c, "y"),
+                                        _rows(dh_out, shape, s, "dh_out"), _rows(dn, shape, c, "dn"), grads,
+                                        _stream(stream)))
+
+
+def _route_desc(logits, index, weights, sigmoid, groups, top_groups, group_best, renormalize, scale, names):
+    shape = _two(logits, "logits")
+    tokens, experts = shape
+    chosen = _two(index, "index")
+    _count(max(experts, chosen[1]), "logits and index")
+    _want(chosen[0] == tokens, f"index has {chosen[0]} rows, expected {tokens}")
+    d = sdp_route_desc(tokens, experts, chosen[1], _type(logits, "logits"), _type(index, "index"),
+                       _type(weights, names), 1 if sigmoid else 0, 1 if renormalize else 0, groups, top_groups,
+                       group_best, scale, _row_stride(logits, shape, "logits"))
+    return d, _dense(index, chosen, "index"), _dense(weights, chosen, names)
+
+
+def sdp_route(ctx, logits, index, weights, *, bias=None, sigmoid: bool = False, groups: int = 1, top_groups: int = 1,
+              group_best: int = 1, renormalize: bool = False, scale: float = 1.0, stream=None) -> None:
+    d, i, w = _route_desc(logits, index, weights, sigmoid, groups, top_groups, group_best, renormalize, scale, "weights")
+    b = None if bias is None else _f32(bias, (d.experts,), "bias")
+    _check(_lib.sdp_route(ctx, d, logits.data_ptr(), b, i, w, _stream(stream)))
+
+
+def sdp_route_backward(ctx, logits, index, dweights, dlogits, *, sigmoid: bool = False, renormalize: bool = False,
+                       scale: float = 1.0, stream=None) -> None:
+    d, i, w = _route_desc(logits, index, dweights, sigmoid, 1, 1, 1, renormalize, scale, "dweights")
+    _same_type(dlogits, d.logit_type, "dlogits")
+    _check(_lib.sdp_route_backward(ctx, d, logits.data_ptr(), i, w, dlogits.data_ptr(),
+                                   _row_stride(dlogits, logits.shape, "dlogits"), _stream(stream)))
+
+
+def sdp_expert_order(ctx, index, ends, place, order=None, *, stream=None) -> None:
+    """index, place: [tokens, top] or [entries]; order: [entries], or None."""
+    experts = ends.shape
+    _want(len(experts) == 1, "ends must be 1-D")
+    _count(experts[0], "ends")
+    n = index.numel()
+    _same_type(place, SDP_TYPE_I32, "place")
+    _same_type(order, SDP_TYPE_I32, "order")
+    d = sdp_order_desc(n, experts[0], _type(index, "index"), _type(ends, "ends"))
+    _check(_lib.sdp_expert_order(ctx, d, _dense(index, index.shape, "index"), _dense(ends, experts, "ends"),
+                                 _dense(place, index.shape, "place"), _dense(order, (n,), "order"), _stream(stream)))
+
+
+def _expert_desc(place, hidden: int, row_type: int, stream_type: int, weight_type: int):
+    tokens, top = _two(place, "place")
+    _count(max(tokens, top, hidden), "place and the rows")
+    _same_type(place, SDP_TYPE_I32, "place")
+    return sdp_expert_desc(tokens, top, hidden, row_type, stream_type, weight_type,
+                           _dense(place, place.shape, "place")), (tokens, hidden), (tokens * top, hidden)
+
+
+def sdp_expert_gather(ctx, x, place, rows, *, stream=None) -> None:
+    code = _type(x, "x")
+    d, side, all_rows = _expert_desc(place, _two(x, "x")[1], code, code, SDP_TYPE_F32)
+    _check(_lib.sdp_expert_gather(ctx, d, _rows(x, side, code, "x"), _rows(rows, all_rows, code, "rows"),
+                                  _stream(stream)))
+
+
+def sdp_expert_gather_backward(ctx, drows, place, dx, *, stream=None) -> None:
+    code = _type(drows, "drows")
+    d, side, all_rows = _expert_desc(place, _two(drows, "drows")[1], code, code, SDP_TYPE_F32)
+    _check(_lib.sdp_expert_gather_backward(ctx, d, _rows(drows, all_rows, code, "drows"), _rows(dx, side, code, "dx"),
+                                           _stream(stream)))
+
+
+def sdp_expert_combine(ctx, rows, place, weights, out, *, residual=None, stream=None) -> None:
+    code, to = _type(rows, "rows"), _type(out, "out")
+    d, side, all_rows = _expert_desc(place, _two(rows, "rows")[1], code, to, _type(weights, "weights"))
+    _check(_lib.sdp_expert_combine(ctx, d, _rows(rows, all_rows, code, "rows"), _dense(weights, place.shape, "weights"),
+                                   _rows(residual, side, to, "residual"), _rows(out, side, to, "out"),
+                                   _stream(stream)))
+
+
+def sdp_expert_combine_backward(ctx, rows, place, weights, dout, drows=None, dweights=None, *, stream=None) -> None:
+    """drows or dweights may be None; rows without dweights, weights without drows."""
+    some = drows if rows is None else rows
+    code, to = _type(dout if some is None else some, "rows"), _type(dout, "dout")
+    w = dweights if weights is None else weights
+    d, side, all_rows = _expert_desc(place, _two(dout, "dout")[1], code, to,
+                                     SDP_TYPE_F32 if w is None else _type(w, "weights"))
+    _same_type(dweights, d.weight_type, "dweights")
+    _check(_lib.sdp_expert_combine_backward(
+        ctx, d, _rows(rows, all_rows, code, "rows"), _dense(weights, place.shape, "weights"),
+        _rows(dout, side, to, "dout"), _rows(drows, all_rows, code, "drows"),
+        _dense(dweights, place.shape, "dweights"), _stream(stream)))
