@@ -269,16 +269,16 @@ int sdp_block_norm_backward(sdp_ctx *ctx, const sdp_block_norm_desc *desc, const
         a.dgate_stride = g.dgate_stride;
         a.dpost = g.dpost_weight;
         a.dpre = g.dpre_weight;
-        const bool wanted[3] = {g.dpre_weight != nullptr, g.dpost_weight != nullptr,
-                                g.dgate && desc->gate_form == SDP_GATE_CHANNEL};
+        const bool wanted[2] = {g.dpre_weight != nullptr,
+                                g.dpost_weight || (g.dgate && desc->gate_form == SDP_GATE_CHANNEL)};
         hipStream_t s = (hipStream_t)stream;
         a.blocks = norm_blocks(a);
-        const int sums = wanted[0] + wanted[1] + wanted[2];
+        const int sums = wanted[0] + wanted[1];
         if (sums) {
             const size_t row = ((size_t)n + 3) / 4 * 4;
             SDP_TRY(take_ops_space(ctx, call, row * std::max(1, a.blocks) * sums * sizeof(float), s));
             float *at = (float *)ctx->ops_space;
-            for (int k = 0; k < 3; ++k)
+            for (int k = 0; k < 2; ++k)
                 if (wanted[k]) a.sums[k] = at, at += row * std::max(1, a.blocks);
         }
         HIP_TRY(launch_norm_backward(a, desc->stream_type == SDP_TYPE_BF16, desc->type == SDP_TYPE_BF16, s));

@@ -83,9 +83,11 @@ struct NormArgs {
     void *dgate;
     int64_t dgate_stride;
     void *dpost, *dpre;
-    // partial sums over tokens, [blocks, hidden] each: dpre, dpost, dgate of channels; NULL: not wanted
-    float *sums[3];
+    // partial sums over tokens, [blocks, hidden] each, of dn h r (for dpre) and of y ry g, times
+    // the gate where it is a token's own (for dpost and the channels' dgate); NULL: not wanted
+    float *sums[2];
     int32_t blocks;
+    int32_t team;  // lanes to a row (set by the launch)
 };
 
 // Blocks of the backward call, each of which leaves a row of partial sums.
