@@ -3,10 +3,11 @@
 //   out[t] = s table[id_t];   dtable[v] = s sum over t with id_t = v of dout[t]
 // Memory bounds both: the tokens' rows, and backward the whole table where it is
 // written anew.  Backward the tokens are sorted by id (sdp_order.hip), so that each
-// row of the table is one run of them, summed in the tokens' order and written once.
-// Runs are cut at every 64th place: where one id fills all 64, their sum is made
-// beforehand, by a wave of its own.
+// row of the table is one run of them.  Waves take pieces of 64 places: a run within a
+// piece is summed and written at once, of a longer one each piece leaves its sum, and
+// the kernel that writes the rest of the table adds those in their order.
 #include <algorithm>
+#include <type_traits>
 
 #include "sdp_layer_device.h"
 #include "sdp_layer_internal.h"
@@ -16,7 +17,7 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kColumns = 512;  // of a wave: eight to a lane
-constexpr int kTableRows = 64; // of a wave, backward
+constexpr int kTableRows = 32;  // of a wave, backward
 
 template <typename T, typename R>
 __global__ __launch_bounds__(64 * kWaves) void k_embed(EmbedArgs a, int slices) {
@@ -39,36 +40,80 @@ __global__ __launch_bounds__(64 * kWaves) void k_embed(EmbedArgs a, int slices) 
     }
 }
 
-// Adds the rows of the tokens at places p0..p1 - 1.
-template <typename R>
-__device__ __forceinline__ void add_places(const EmbedArgs &a, int64_t p0, int64_t p1, int c, int left, float *sum) {
-    for (int64_t p = p0; p < p1; ++p) {
-        float v[8];
-        load_floats((const R *)a.rows.data + (int64_t)a.order[p] * a.rows.stride + c, left, v);
+// A row of the table's gradient: eight columns of it.
+template <typename T, bool ONCE>
+__device__ __forceinline__ void put_row(const EmbedArgs &a, int64_t v, int c, int left, float *sum) {
+    T *out = (T *)a.table.data + v * a.table.stride + c;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) sum[k] += v[k];
+    for (int k = 0; k < 8; ++k) sum[k] *= a.scale;
+    if (a.accumulate) {
+        float x[8];
+        load_floats(out, left, x);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum[k] += x[k];
+    }
+    store_floats<ONCE>(out, left, sum);
+}
+
+// A wave takes 512 columns of a piece's places.
+template <typename T, typename R, bool ONCE>
+__device__ __forceinline__ void add_piece(const EmbedArgs &a, int64_t piece, int c) {
+    constexpr int kAhead = 8;
+    const int lane = threadIdx.x & 63, left = a.hidden - c;
+    const int64_t p0 = piece * kEmbedPiece, n = a.tokens;
+    // lane l has the piece's l-th place
+    const bool on = p0 + lane < n;
+    const int32_t my_key = on ? a.key[p0 + lane] : a.vocab, my_entry = on ? a.order[p0 + lane] : 0;
+    const int32_t key_before = p0 > 0 ? a.key[p0 - 1] : -1, key_after = p0 + 64 < n ? a.key[p0 + 64] : -1;
+    // keys are in order, those of no row of the table last
+    const int count = __popcll(__ballot(my_key < a.vocab));
+    float sum[8] = {};
+    bool first = true;  // the piece's first run
+    Eight<R> x[kAhead];
+    auto fetch = [&](int i) __attribute__((always_inline)) {
+        const int64_t t = __builtin_amdgcn_readlane(my_entry, i & 63);
+        return load_eight<ONCE>((const R *)a.rows.data + t * a.rows.stride + c, i < count ? left : 0);
+    };
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) x[u] = fetch(u);
+    for (int i = 0; i < count; i += kAhead) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (i + u >= count) break;
+            const int32_t id = __builtin_amdgcn_readlane(my_key, i + u);
+            const bool ends = i + u == 63,
+                       last = i + u + 1 == count || __builtin_amdgcn_readlane(my_key, (i + u + 1) & 63) != id;
+            float v[8];
+            x[u].floats(v);
+            x[u] = fetch(i + u + kAhead);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum[k] += v[k];
+            if (!last) continue;
+            if (first && key_before == id)
+                store_floats(a.sums + (2 * piece) * a.hidden + c, left, sum);
+            else if (ends && key_after == id)
+                store_floats(a.sums + (2 * piece + 1) * a.hidden + c, left, sum);
+            else if (left > 0)
+                put_row<T, ONCE>(a, id, c, left, sum);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum[k] = 0.0f;
+            first = false;
+        }
     }
 }
 
-// The sums of aligned runs of places that one id fills.
-template <typename R>
-__global__ __launch_bounds__(64 * kWaves) void k_embed_runs(EmbedArgs a, int slices) {
-    const int lane = threadIdx.x & 63;
-    const int64_t runs = a.tokens / kEmbedRun;
-    for (int64_t w = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6); w < runs * slices;
+template <typename T, typename R, bool ONCE>
+__global__ __launch_bounds__(64 * kWaves) void k_embed_pieces(EmbedArgs a, int slices) {
+    const int64_t waves = (a.tokens + kEmbedPiece - 1) / kEmbedPiece * slices;
+    for (int64_t w = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); w < waves;
          w += (int64_t)gridDim.x * kWaves) {
-        const int64_t run = w / slices, p = run * kEmbedRun;
-        const int c = (int)(w - run * slices) * kColumns + lane * 8, left = a.hidden - c;
-        const int32_t id = a.key[p];
-        if (id != a.key[p + kEmbedRun - 1] || id >= a.vocab || left <= 0) continue;
-        float sum[8] = {};
-        add_places<R>(a, p, p + kEmbedRun, c, left, sum);
-        store_floats(a.runs + run * a.hidden + c, left, sum);
+        const int64_t piece = w / slices;
+        add_piece<T, R, ONCE>(a, piece, (int)(w - piece * slices) * kColumns + (threadIdx.x & 63) * 8);
     }
 }
 
 // The first place whose key is v or more.
-__device__ __forceinline__ int64_t lower_bound(const EmbedArgs &a, int32_t v) {
+__device__ __forceinline__ int64_t lower_bound(const EmbedArgs &a, int64_t v) {
     int64_t lo = 0, hi = a.tokens;
     while (lo < hi) {
         const int64_t mid = (lo + hi) / 2;
@@ -80,48 +125,42 @@ __device__ __forceinline__ int64_t lower_bound(const EmbedArgs &a, int32_t v) {
     return lo;
 }
 
-template <typename T, typename R>
-__global__ __launch_bounds__(64 * kWaves) void k_embed_table(EmbedArgs a, int slices) {
+// What the pieces have not written: rows of no token, and of runs over several pieces.
+// A block takes 32 rows, a thread eight columns of each 2,048.
+template <typename T, bool ONCE>
+__global__ __launch_bounds__(64 * kWaves) void k_embed_table(EmbedArgs a) {
+    constexpr int kStride = 64 * kWaves * 8, kAhead = 4;
     const int lane = threadIdx.x & 63;
-    const int64_t parts = ((int64_t)a.vocab + kTableRows - 1) / kTableRows;
-    for (int64_t w = (int64_t)blockIdx.x * kWaves + (threadIdx.x >> 6); w < parts * slices;
-         w += (int64_t)gridDim.x * kWaves) {
-        const int64_t part = w / slices;
-        const int c = (int)(w - part * slices) * kColumns + lane * 8, left = a.hidden - c;
-        const int64_t v0 = part * kTableRows, v1 = v0 + kTableRows < a.vocab ? v0 + kTableRows : a.vocab;
-        const int64_t mine = v0 + lane + 1;
-        // lane l has the end of row v0 + l
-        const int64_t end = lower_bound(a, (int32_t)(mine < v1 ? mine : v1));
-        int64_t p0 = lower_bound(a, (int32_t)v0);
+    for (int64_t v0 = (int64_t)blockIdx.x * kTableRows; v0 < a.vocab; v0 += (int64_t)gridDim.x * kTableRows) {
+        const int64_t v1 = min(v0 + kTableRows, (int64_t)a.vocab);
+        // lane l has the first place of row v0 + l
+        const int mine = (int)lower_bound(a, min(v0 + lane, v1));
         for (int64_t v = v0; v < v1; ++v) {
-            const int64_t p1 = __shfl(end, (int)(v - v0));
-            if (left > 0 && (p1 > p0 || !a.accumulate)) {
+            const int p0 = __builtin_amdgcn_readlane(mine, (int)(v - v0)),
+                      p1 = __builtin_amdgcn_readlane(mine, (int)(v - v0 + 1));
+            const int r0 = p0 / kEmbedPiece, r1 = (p1 - 1) / kEmbedPiece;
+            if (p0 == p1 ? a.accumulate : r0 == r1) continue;
+            for (int c = threadIdx.x * 8; c < a.hidden; c += kStride) {
+                const int left = a.hidden - c;
                 float sum[8] = {};
-                const int64_t r0 = (p0 + kEmbedRun - 1) / kEmbedRun, r1 = p1 / kEmbedRun;
-                if (r1 > r0) {
-                    add_places<R>(a, p0, r0 * kEmbedRun, c, left, sum);
-                    for (int64_t r = r0; r < r1; ++r) {
-                        float x[8];
-                        load_floats(a.runs + r * a.hidden + c, left, x);
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) sum[k] += x[k];
-                    }
-                    add_places<R>(a, r1 * kEmbedRun, p1, c, left, sum);
-                } else {
-                    add_places<R>(a, p0, p1, c, left, sum);
+                if (p0 == p1) {
+                    store_floats<ONCE>((T *)a.table.data + v * a.table.stride + c, left, sum);
+                    continue;
                 }
+                for (int r = r0; r <= r1; r += kAhead) {
+                    float x[kAhead][8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) sum[k] *= a.scale;
-                T *out = (T *)a.table.data + v * a.table.stride + c;
-                if (a.accumulate) {
-                    float x[8];
-                    load_floats(out, left, x);
+                    for (int u = 0; u < kAhead; ++u)
+                        // in its first piece the run comes last
+                        load_floats(a.sums + (2 * (int64_t)min(r + u, r1) + (r + u == r0 ? 1 : 0)) * a.hidden + c, left,
+                                    x[u]);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) sum[k] += x[k];
+                    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) sum[k] += r + u <= r1 ? x[u][k] : 0.0f;
                 }
-                store_floats(out, left, sum);
+                put_row<T, ONCE>(a, v, c, left, sum);
             }
-            p0 = p1;
         }
     }
 }
@@ -161,11 +200,9 @@ size_t embed_workspace(EmbedArgs &a, char *space) {
         return p;
     };
     const SortArgs s = sort_args(a);
-    a.order = (int32_t *)part((size_t)a.tokens * 4);
-    a.spare = (int32_t *)part((size_t)a.tokens * 4);
-    a.key = (int32_t *)part((size_t)a.tokens * 4);
-    a.counts = (int32_t *)part((size_t)s.blocks * s.digits * 4);
-    a.runs = (float *)part((size_t)(a.tokens / kEmbedRun) * a.hidden * 4);
+    for (int32_t **p : {&a.order, &a.order_spare, &a.key, &a.key_spare}) *p = (int32_t *)part((size_t)a.tokens * 4);
+    a.counts = sort_needs_counts(s) ? (int32_t *)part((size_t)s.blocks * s.digits * 4) : nullptr;
+    a.sums = (float *)part(((size_t)a.tokens + kEmbedPiece - 1) / kEmbedPiece * 2 * a.hidden * 4);
     return at + 256;
 }
 
@@ -190,28 +227,36 @@ hipError_t launch_embed_backward(const EmbedArgs &args, bool table_bf16, bool ro
     const int bits = key_bits(a);
     for (int shift = 0; shift < bits && a.tokens > 0; shift += sort.bits) {
         sort.shift = shift;
-        sort.order_in = shift ? a.order : nullptr;
-        sort.order_out = a.spare;
-        sort.keys_out = shift + sort.bits >= bits ? a.key : nullptr;
+        if (shift) sort.keys = a.key, sort.keys64 = 0, sort.order_in = a.order;
+        sort.order_out = a.order_spare;
+        sort.keys_out = a.key_spare;
         const hipError_t e = launch_sort(sort, s);
         if (e != hipSuccess) return e;
-        std::swap(a.order, a.spare);
+        std::swap(a.order, a.order_spare);
+        std::swap(a.key, a.key_spare);
     }
-    if (a.tokens >= kEmbedRun) {
-        const dim3 grid(grid_of(a.tokens / kEmbedRun * slices));
-        if (rows_bf16)
-            hipLaunchKernelGGL((k_embed_runs<uint16_t>), grid, dim3(64 * kWaves), 0, s, a, slices);
-        else
-            hipLaunchKernelGGL((k_embed_runs<float>), grid, dim3(64 * kWaves), 0, s, a, slices);
+    // past the last-level cache
+    const bool once = a.tokens * a.hidden * (rows_bf16 ? 2 : 4) +
+                          (a.accumulate ? 0 : (int64_t)a.vocab * a.hidden * (table_bf16 ? 2 : 4)) >
+                      (int64_t)256 << 20;
+    if (a.tokens > 0) {
+        const dim3 grid(grid_of((a.tokens + kEmbedPiece - 1) / kEmbedPiece * slices));
+        auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kWaves), 0, s, a, slices); };
+        auto pick = [&](auto is_once) {
+            constexpr bool O = decltype(is_once)::value;
+            if (table_bf16)
+                rows_bf16 ? go(k_embed_pieces<uint16_t, uint16_t, O>) : go(k_embed_pieces<uint16_t, float, O>);
+            else
+                rows_bf16 ? go(k_embed_pieces<float, uint16_t, O>) : go(k_embed_pieces<float, float, O>);
+        };
+        once ? pick(std::true_type()) : pick(std::false_type());
     }
-    const int64_t waves = ((int64_t)a.vocab + kTableRows - 1) / kTableRows * slices;
-    auto go = [&](auto kernel) {
-        hipLaunchKernelGGL(kernel, dim3(grid_of(waves)), dim3(64 * kWaves), 0, s, a, slices);
-    };
+    const dim3 grid((uint32_t)std::min<int64_t>(((int64_t)a.vocab + kTableRows - 1) / kTableRows, 1 << 20));
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kWaves), 0, s, a); };
     if (table_bf16)
-        rows_bf16 ? go(k_embed_table<uint16_t, uint16_t>) : go(k_embed_table<uint16_t, float>);
+        once ? go(k_embed_table<uint16_t, true>) : go(k_embed_table<uint16_t, false>);
     else
-        rows_bf16 ? go(k_embed_table<float, uint16_t>) : go(k_embed_table<float, float>);
+        once ? go(k_embed_table<float, true>) : go(k_embed_table<float, false>);
     return hipGetLastError();
 }
 

@@ -23,7 +23,7 @@ struct Rows {
 // One pass of a stable counting sort: n entries by digits in [0, digits).  The
 // counts of each block of entries lie in a row of `digits` of their own.
 struct SortArgs {
-    const void *keys;         // [n] expert indexes or token ids
+    const void *keys;         // [n] expert indexes or token ids, in the order before the pass
     int32_t keys64;
     int32_t limit;            // keys outside 0..limit - 1 count as limit
     int64_t n;
@@ -44,6 +44,7 @@ struct SortArgs {
 
 // How the entries are split over blocks; counts may be place itself, rows a chunk apart.
 void sort_split(SortArgs &a);
+bool sort_needs_counts(const SortArgs &a);
 hipError_t launch_sort(const SortArgs &a, hipStream_t s);
 
 // ---- embeddings ----------------------------------------------------------------
@@ -58,11 +59,13 @@ struct EmbedArgs {
     Rows rows;   // out, or dout
     int32_t accumulate;
     // workspace of the gradient
-    int32_t *order, *spare, *key, *counts;
-    float *runs;  // sums of the aligned runs of kEmbedRun places that one id fills
+    int32_t *order, *order_spare, *key, *key_spare, *counts;
+    // [pieces, 2, hidden] sums of what a piece of kEmbedPiece places has of ids that go on
+    // before it (or all through it) and of ids that go on behind it
+    float *sums;
 };
 
-constexpr int kEmbedRun = 64;
+constexpr int kEmbedPiece = 64;
 
 size_t embed_workspace(EmbedArgs &a, char *space);
 hipError_t launch_embed(const EmbedArgs &a, bool table_bf16, bool rows_bf16, hipStream_t s);
