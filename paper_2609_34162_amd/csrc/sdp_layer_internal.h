@@ -113,6 +113,9 @@ struct RouteArgs {
     const void *index_in, *dweights;
     void *dlogits;
     int64_t dlogits_stride;
+    // set by the launch: lanes of a token, and the launch's first wave's worth of tokens
+    int32_t lanes;
+    int64_t first;
 };
 
 hipError_t launch_route(const RouteArgs &a, bool bf16, hipStream_t s);
