@@ -272,7 +272,8 @@ int sdp_block_norm_backward(sdp_ctx *ctx, const sdp_block_norm_desc *desc, const
         const bool wanted[2] = {g.dpre_weight != nullptr,
                                 g.dpost_weight || (g.dgate && desc->gate_form == SDP_GATE_CHANNEL)};
         hipStream_t s = (hipStream_t)stream;
-        a.blocks = norm_blocks(a);
+        const bool stream_bf16 = desc->stream_type == SDP_TYPE_BF16, bf16 = desc->type == SDP_TYPE_BF16;
+        a.blocks = norm_blocks(a, stream_bf16, bf16);
         const int sums = wanted[0] + wanted[1];
         if (sums) {
             const size_t row = ((size_t)n + 3) / 4 * 4;
@@ -281,7 +282,7 @@ int sdp_block_norm_backward(sdp_ctx *ctx, const sdp_block_norm_desc *desc, const
             for (int k = 0; k < 2; ++k)
                 if (wanted[k]) a.sums[k] = at, at += row * std::max(1, a.blocks);
         }
-        HIP_TRY(launch_norm_backward(a, desc->stream_type == SDP_TYPE_BF16, desc->type == SDP_TYPE_BF16, s));
+        HIP_TRY(launch_norm_backward(a, stream_bf16, bf16, s));
         return sums ? ops_mark(ctx, s) : SDP_OK;
     });
 }

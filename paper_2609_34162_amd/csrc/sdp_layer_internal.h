@@ -94,7 +94,7 @@ struct NormArgs {
 };
 
 // Blocks of the backward call, each of which leaves a row of partial sums.
-int norm_blocks(const NormArgs &a);
+int norm_blocks(const NormArgs &a, bool stream_bf16, bool bf16);
 hipError_t launch_norm(const NormArgs &a, bool stream_bf16, bool bf16, hipStream_t s);
 hipError_t launch_norm_backward(const NormArgs &a, bool stream_bf16, bool bf16, hipStream_t s);
 

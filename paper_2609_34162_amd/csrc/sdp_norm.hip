@@ -23,17 +23,23 @@ __device__ __forceinline__ float weight_at(const NormArgs &a, const void *w, int
     return w ? a.offset + load_either(w, i, a.weight_bf16) : 1.0f;
 }
 
-// The gate of an element, and its slope by the gate's input.
+// A gate after its activation, and its slope by the gate's input: of a sigmoid s the slope
+// is s (1 - s) = s^2 e, e = exp(-z), which loses nothing where s is close to one.
+struct Gate {
+    float act, slope;
+};
+__device__ __forceinline__ Gate gate_of(const NormArgs &a, float z) {
+    if (!a.sigmoid) return {z, 1.0f};
+    const float e = fminf(expf(-z), __FLT_MAX__), s = __builtin_amdgcn_rcpf(1.0f + e);
+    return {z != z ? z : s, s * (s * e)};
+}
+
+// The gate of an element (or 1).
 template <typename T>
-__device__ __forceinline__ float gate_at(const NormArgs &a, int64_t t, int64_t i, float *slope) {
-    *slope = 1.0f;
-    if (a.gate_form == SDP_GATE_NONE) return 1.0f;
+__device__ __forceinline__ Gate gate_at(const NormArgs &a, int64_t t, int64_t i) {
+    if (a.gate_form == SDP_GATE_NONE) return {1.0f, 1.0f};
     const int64_t at = a.gate_form == SDP_GATE_CHANNEL ? i : t * a.gate_stride + (a.gate_form == SDP_GATE_ELEMENT ? i : 0);
-    const float z = load1((const T *)a.gate + at);
-    if (!a.sigmoid) return z;
-    const float g = 1.0f / (1.0f + expf(-z));
-    *slope = g * (1.0f / (1.0f + expf(z)));
-    return g;
+    return gate_of(a, load1((const T *)a.gate + at));
 }
 
 __device__ __forceinline__ float block_sum(float v, float *waves) {
@@ -67,10 +73,10 @@ __global__ __launch_bounds__(kThreads) void k_norm_any(NormArgs a) {
             ry = rsqrtf(block_sum(sq, waves) * inv + a.eps);
         }
         auto sum_at = [&](int64_t i) {
-            float v = load1(h + i), slope;
+            float v = load1(h + i);
             if (y) {
                 const float u = a.post_norm ? load1(y + i) * ry * weight_at(a, a.post_weight, i) : load1(y + i);
-                v += a.scale * gate_at<T>(a, t, i, &slope) * u;
+                v += a.scale * gate_at<T>(a, t, i).act * u;
             }
             return v;
         };
@@ -132,22 +138,20 @@ __global__ __launch_bounds__(kThreads) void k_norm_back_any(NormArgs a) {
         };
         float dot = 0.0f;
         if (a.post_norm && a.dy.data) {
-            for (int64_t i = threadIdx.x; i < a.hidden; i += kThreads) {
-                float slope;
-                dot += a.scale * gate_at<T>(a, t, i, &slope) * g_at(i) * weight_at(a, a.post_weight, i) * load1(y + i);
-            }
+            for (int64_t i = threadIdx.x; i < a.hidden; i += kThreads)
+                dot += a.scale * gate_at<T>(a, t, i).act * g_at(i) * weight_at(a, a.post_weight, i) * load1(y + i);
             dot = block_sum(dot, waves) * inv * ry * ry;
         }
         float gate_sum = 0.0f;
         for (int64_t i = threadIdx.x; i < a.hidden; i += kThreads) {
             const float g = g_at(i);
-            float slope;
-            const float act = gate_at<T>(a, t, i, &slope), du = a.scale * act * g;
+            const Gate gate = gate_at<T>(a, t, i);
+            const float du = a.scale * gate.act * g;
             const float x = y ? load1(y + i) : 0.0f, w = a.post_norm ? weight_at(a, a.post_weight, i) : 1.0f;
             if (sums[0]) sums[0][i] += load1(dn + i) * load1(h + i) * r;
-            if (sums[1]) sums[1][i] += (a.gate_form >= SDP_GATE_TOKEN ? act : 1.0f) * x * ry * g;
+            if (sums[1]) sums[1][i] += (a.gate_form >= SDP_GATE_TOKEN ? gate.act : 1.0f) * x * ry * g;
             if (a.dgate) {
-                const float d = a.scale * (x * ry * w) * g * slope;
+                const float d = a.scale * (x * ry * w) * g * gate.slope;
                 if (a.gate_form == SDP_GATE_ELEMENT) store1((T *)a.dgate + t * a.dgate_stride + i, d);
                 gate_sum += d;
             }
@@ -210,11 +214,6 @@ __device__ __forceinline__ void team_sums(float *v, int team, float (*waves)[kMo
     for (int k = 0; k < N; ++k) v[k] = lanes_sum(from < wave_count ? waves[k][from] : 0.0f, kMostWaves);
 }
 
-template <typename T>
-__device__ __forceinline__ float activated(const NormArgs &a, float z) {
-    return a.sigmoid ? 1.0f / (1.0f + expf(-z)) : z;
-}
-
 // NV 2: the next row is not loaded ahead, for want of registers.
 template <typename S, typename T, int NV, bool WIDE, bool ONCE, int THREADS>
 __global__ __launch_bounds__(THREADS) void k_norm_rows(NormArgs a) {
@@ -233,7 +232,7 @@ __global__ __launch_bounds__(THREADS) void k_norm_rows(NormArgs a) {
         for (int k = 0; k < 8; ++k) {
             const bool in = k < left[j];
             add[j][k] = in ? a.scale * (a.post_norm ? weight_at(a, a.post_weight, c[j] + k) : 1.0f) : 0.0f;
-            if (in && a.gate_form == SDP_GATE_CHANNEL) add[j][k] *= activated<T>(a, load1((const T *)a.gate + c[j] + k));
+            if (in && a.gate_form == SDP_GATE_CHANNEL) add[j][k] *= gate_of(a, load1((const T *)a.gate + c[j] + k)).act;
             pre[j][k] = in ? weight_at(a, a.pre_weight, c[j] + k) : 0.0f;
         }
     }
@@ -272,10 +271,10 @@ __global__ __launch_bounds__(THREADS) void k_norm_rows(NormArgs a) {
                 float z[8];
                 gate[j].floats(z);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) u[j][k] *= activated<T>(a, z[k]);
+                for (int k = 0; k < 8; ++k) u[j][k] *= gate_of(a, z[k]).act;
             }
         }
-        if (a.gate_form == SDP_GATE_TOKEN) factor = activated<T>(a, token_gate);
+        if (a.gate_form == SDP_GATE_TOKEN) factor = gate_of(a, token_gate).act;
         if (kAhead && t + at.teams < a.tokens) fetch(t + at.teams);
         if (has_y && a.post_norm) {
             team_sums<1, WIDE>(&sq, a.team, waves[parity][0], wave_count);
@@ -334,12 +333,11 @@ __global__ __launch_bounds__(THREADS) void k_norm_back_rows(NormArgs a) {
     for (int k = 0; k < 8; ++k) {
         const bool in = k < left;
         q[k] = in ? a.scale * (a.post_norm ? weight_at(a, a.post_weight, c + k) : 1.0f) : 0.0f;
-        if (in && a.gate_form == SDP_GATE_CHANNEL) q[k] *= activated<T>(a, load1((const T *)a.gate + c + k));
+        if (in && a.gate_form == SDP_GATE_CHANNEL) q[k] *= gate_of(a, load1((const T *)a.gate + c + k)).act;
         pre[k] = in ? weight_at(a, a.pre_weight, c + k) : 0.0f;
         sum_n[k] = sum_y[k] = 0.0f;
     }
     BackRow<S, T> row;
-    float token_gate = 1.0f;
     auto fetch = [&](int64_t t, BackRow<S, T> &to) __attribute__((always_inline)) {
         if (left > 0) {
             if (has_n) {
@@ -368,12 +366,8 @@ __global__ __launch_bounds__(THREADS) void k_norm_back_rows(NormArgs a) {
         } else if (on) {
             fetch(t, row);
         }
-        float act = 1.0f, slope = 1.0f;
-        if (by_token && on) {
-            token_gate = load1((const T *)a.gate + t * a.gate_stride);
-            act = activated<T>(a, token_gate);
-            if (a.sigmoid) slope = act * (1.0f / (1.0f + expf(token_gate)));
-        }
+        Gate of_token = {1.0f, 1.0f};
+        if (by_token && on) of_token = gate_of(a, load1((const T *)a.gate + t * a.gate_stride));
         float s[6] = {};
         {
             float x[8], v[8], g[8], z[8], f[8];
@@ -386,7 +380,7 @@ __global__ __launch_bounds__(THREADS) void k_norm_back_rows(NormArgs a) {
                 s[1] += vw * x[k];
                 s[2] += z[k] * z[k];
                 float qy = q[k] * z[k];
-                if (EACH) qy *= activated<T>(a, f[k]);
+                if (EACH) qy *= gate_of(a, f[k]).act;
                 s[3] += qy * g[k];
                 s[4] += qy * vw;
                 s[5] += qy * x[k];
@@ -402,8 +396,8 @@ __global__ __launch_bounds__(THREADS) void k_norm_back_rows(NormArgs a) {
         }
         if (a.post_norm && has_y) ry = rsqrtf(s[2] * inv + a.eps);
         if (dots) dot = s[3] + r * (s[4] - along * s[5]);  // sum of q y g
-        if (by_token && a.dgate && on && at.lane == 0) store1((T *)a.dgate + t * a.dgate_stride, slope * ry * dot);
-        const float back = a.post_norm ? act * dot * inv * ry * ry : 0.0f;
+        if (by_token && a.dgate && on && at.lane == 0) store1((T *)a.dgate + t * a.dgate_stride, of_token.slope * ry * dot);
+        const float back = a.post_norm ? of_token.act * dot * inv * ry * ry : 0.0f;
         if (!on) continue;
         float x[8], v[8], g[8], z[8], f[8];
         row.h.floats(x), row.dn.floats(v), row.dh.floats(g), row.y.floats(z);
@@ -413,10 +407,11 @@ __global__ __launch_bounds__(THREADS) void k_norm_back_rows(NormArgs a) {
             const float gk = g[k] + r * (v[k] * pre[k] - x[k] * along);
             g[k] = gk;
             const float yg = z[k] * ry * gk;
-            float mine = act;
+            float mine = of_token.act;
             if (EACH) {
-                mine = activated<T>(a, f[k]);
-                f[k] = q[k] * yg * (a.sigmoid ? mine * (1.0f / (1.0f + expf(f[k]))) : 1.0f);
+                const Gate of = gate_of(a, f[k]);
+                mine = of.act;
+                f[k] = q[k] * yg * of.slope;
             }
             sum_n[k] += v[k] * x[k] * r;
             sum_y[k] += mine * yg;
@@ -448,18 +443,19 @@ __global__ __launch_bounds__(THREADS) void k_norm_back_rows(NormArgs a) {
     }
 }
 
-// The blocks' partial sums, added in their order: 64 channels to a block, 16 threads
-// of four channels to a row of them, 64 rows at a time.  blockIdx.y: which sums.
-constexpr int kSumThreads = 1024, kSumRows = kSumThreads / 16;
+// The blocks' partial sums, added in their order: 32 channels to a block, eight threads
+// of four channels to a row of them, 128 rows at a time.  blockIdx.y: which sums.
+constexpr int kSumThreads = 1024, kSumLanes = 8, kSumRows = kSumThreads / kSumLanes;
 template <typename T>
 __global__ __launch_bounds__(kSumThreads) void k_norm_sums(NormArgs a) {
-    __shared__ f32x4 part[kSumRows][16];
-    const int which = blockIdx.y, x = threadIdx.x & 15, y = threadIdx.x >> 4;
+    __shared__ f32x4 part[kSumRows][kSumLanes];
+    const int which = blockIdx.y, x = threadIdx.x % kSumLanes, y = threadIdx.x / kSumLanes;
     if (!a.sums[which]) return;
-    const int64_t i = (int64_t)blockIdx.x * 64 + x * 4;
+    const int64_t i = ((int64_t)blockIdx.x * kSumLanes + x) * 4;
     f32x4 s = {0.0f, 0.0f, 0.0f, 0.0f};
     if (i < a.hidden) {
         const float *from = a.sums[which] + i;
+#pragma unroll 4
         for (int b = y; b < a.blocks; b += kSumRows) s += *(const f32x4 *)(from + b * sums_stride(a));
     }
     part[y][x] = s;
@@ -480,13 +476,12 @@ __global__ __launch_bounds__(kSumThreads) void k_norm_sums(NormArgs a) {
             put(a.dpre, s[k]);
             continue;
         }
-        float slope;
         const bool channel = a.gate_form == SDP_GATE_CHANNEL;
-        const float act = channel ? gate_at<T>(a, 0, i + k, &slope) : 1.0f;
-        if (a.dpost) put(a.dpost, a.scale * act * s[k]);
+        const Gate gate = channel ? gate_at<T>(a, 0, i + k) : Gate{1.0f, 1.0f};
+        if (a.dpost) put(a.dpost, a.scale * gate.act * s[k]);
         if (a.dgate && channel)
             store1((T *)a.dgate + i + k,
-                   a.scale * slope * (a.post_norm ? weight_at(a, a.post_weight, i + k) : 1.0f) * s[k]);
+                   a.scale * gate.slope * (a.post_norm ? weight_at(a, a.post_weight, i + k) : 1.0f) * s[k]);
     }
 }
 
@@ -517,10 +512,15 @@ Split split_of(const NormArgs &a, bool backward) {
     return {0, kThreads, 1};
 }
 
-// Blocks that a call's rows are walked by: enough to fill the compute units once.
-int blocks_of(const NormArgs &a, const Split &s, bool backward) {
-    const int64_t per = s.team ? s.threads / s.team : 1, most = s.team ? 256 * (2048 / s.threads) : 1024;
-    return (int)std::min<int64_t>((a.tokens + per - 1) / per, backward ? std::min<int64_t>(most, 1024) : most);
+// Blocks that a call's rows are walked by: at most as many as the compute units hold at
+// once (forward eight waves to a SIMD, or what is left of them; backward three, or four of
+// 16-bit tensors), and each as many rows as the others.
+int blocks_of(const NormArgs &a, const Split &s, bool backward, bool wide_types) {
+    const int64_t per = s.team ? s.threads / s.team : 1, waves = s.threads / 64;
+    const int64_t held = !backward ? 32 : wide_types ? 12 : 16;
+    const int64_t most = 256 * (s.team ? std::max<int64_t>(1, held / waves) : 4);
+    const int64_t rows = (a.tokens + per - 1) / per, each = (rows + most - 1) / most;
+    return (int)((rows + each - 1) / each);
 }
 
 // Whether a call's tensors are past the last-level cache.
@@ -528,13 +528,15 @@ bool past_cache(const NormArgs &a, int64_t bytes) { return a.tokens * a.hidden *
 
 }  // namespace
 
-int norm_blocks(const NormArgs &a) { return a.tokens ? blocks_of(a, split_of(a, true), true) : 0; }
+int norm_blocks(const NormArgs &a, bool stream_bf16, bool bf16) {
+    return a.tokens ? blocks_of(a, split_of(a, true), true, !(stream_bf16 && bf16)) : 0;
+}
 
 hipError_t launch_norm(const NormArgs &args, bool stream_bf16, bool bf16, hipStream_t s) {
     NormArgs a = args;
     const Split split = split_of(a, false);
     a.team = split.team;
-    const dim3 grid(blocks_of(a, split, false)), block(split.threads);
+    const dim3 grid(blocks_of(a, split, false, false)), block(split.threads);
     const bool once = past_cache(a, 2 * ((stream_bf16 ? 2 : 4) + (bf16 ? 2 : 4)));
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, block, 0, s, a); };
     with_types(stream_bf16, bf16, [&](auto *st, auto *ty) {
@@ -576,7 +578,7 @@ hipError_t launch_norm_backward(const NormArgs &args, bool stream_bf16, bool bf1
         });
     }
     if (a.sums[0] || a.sums[1]) {
-        const dim3 grid((a.hidden - 1) / 64 + 1, 2);
+        const dim3 grid((a.hidden - 1) / (4 * kSumLanes) + 1, 2);
         if (bf16)
             hipLaunchKernelGGL((k_norm_sums<uint16_t>), grid, dim3(kSumThreads), 0, s, a);
         else

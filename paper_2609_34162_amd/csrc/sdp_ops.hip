@@ -10,7 +10,13 @@ namespace sdpops {
 
 // ---- checks -----------------------------------------------------------------
 
-static int check_memory(const sdp_ctx *ctx, const char *call, const Tensor &t, int64_t bytes) {
+// An allocation that a call's earlier buffers were found to lie in.
+struct Allocation {
+    const char *base;
+    size_t size;
+};
+
+static int check_memory(const sdp_ctx *ctx, const char *call, const Tensor &t, int64_t bytes, Allocation &found) {
     hipPointerAttribute_t at;
     if (hipPointerGetAttributes(&at, t.p) != hipSuccess) {
         (void)hipGetLastError();
@@ -28,14 +34,20 @@ static int check_memory(const sdp_ctx *ctx, const char *call, const Tensor &t, i
     if ((size_t)bytes > size - (size_t)((const char *)t.p - (const char *)base))
         return fail(SDP_ERR_NOT_DEVICE_MEMORY, "%s: %s: %lld bytes at %p overrun its allocation", call, t.what,
                     (long long)bytes, t.p);
+    found = {(const char *)base, size};
     return SDP_OK;
 }
 
 int check_tensors(const sdp_ctx *ctx, const char *call, const std::vector<Tensor> &ts,
                   const std::vector<std::pair<int, int>> &in_place) {
-    for (const Tensor &t : ts) {
+    constexpr size_t kMost = 32;  // more tensors than any call has
+    int64_t bytes[kMost];         // from a tensor's first element to its last
+    if (ts.size() > kMost) return fail(SDP_ERR_INVALID_ARGUMENT, "%s: too many tensors", call);
+    for (size_t i = 0; i < ts.size(); ++i) {
+        const Tensor &t = ts[i];
         const int64_t elems = sdpops::span(t.layout);
         if (elems < 0) return fail(SDP_ERR_INVALID_ARGUMENT, "%s: %s: a stride is negative or too large", call, t.what);
+        bytes[i] = elems * t.size;
         if (elems == 0) continue;
         if (!t.p) return fail(SDP_ERR_INVALID_ARGUMENT, "%s: %s is NULL", call, t.what);
         if ((uintptr_t)t.p % (uintptr_t)t.size != 0)
@@ -44,25 +56,33 @@ int check_tensors(const sdp_ctx *ctx, const char *call, const std::vector<Tensor
         if (t.written && !sdpops::injective(t.layout))
             return fail(SDP_ERR_INVALID_ARGUMENT, "%s: %s overlaps itself", call, t.what);
     }
-    for (const Tensor &t : ts) {
-        const int64_t elems = sdpops::span(t.layout);
-        if (elems > 0) SDP_TRY(check_memory(ctx, call, t, elems * t.size));
+    // a program's small buffers often share an allocation, which is then looked up once
+    Allocation found[4];
+    int founds = 0;
+    for (size_t i = 0; i < ts.size(); ++i) {
+        if (bytes[i] == 0) continue;
+        const char *p = (const char *)ts[i].p;
+        bool known = false;
+        for (int k = 0; k < founds; ++k)
+            known = known || (p >= found[k].base && (size_t)bytes[i] <= found[k].size &&
+                              (size_t)(p - found[k].base) <= found[k].size - (size_t)bytes[i]);
+        if (known) continue;
+        Allocation a;
+        SDP_TRY(check_memory(ctx, call, ts[i], bytes[i], a));
+        if (founds < 4) found[founds++] = a;
     }
     for (size_t i = 0; i < ts.size(); ++i) {
-        if (!ts[i].written) continue;
+        if (!ts[i].written || bytes[i] == 0) continue;
         for (size_t j = 0; j < ts.size(); ++j) {
-            if (i == j || (ts[j].written && j < i)) continue;
+            if (i == j || bytes[j] == 0 || (ts[j].written && j < i)) continue;
             const Tensor &a = ts[i], &b = ts[j];
+            const char *pa = (const char *)a.p, *pb = (const char *)b.p;
+            if (pa + bytes[i] <= pb || pb + bytes[j] <= pa) continue;
             bool may = false;
             for (const auto &pr : in_place)
                 may = may || (pr.first == (int)i && pr.second == (int)j) || (pr.first == (int)j && pr.second == (int)i);
-            if (may && a.size == b.size &&
-                sdpops::same_tensor((const char *)a.p, a.layout, (const char *)b.p, b.layout))
-                continue;
-            const char *pa = (const char *)a.p, *pb = (const char *)b.p;
-            const int64_t na = sdpops::span(a.layout) * a.size, nb = sdpops::span(b.layout) * b.size;
-            const bool apart = na == 0 || nb == 0 || pa + na <= pb || pb + nb <= pa;
-            if (!apart && !(a.size == b.size && sdpops::disjoint(pa, a.layout, pb, b.layout, a.size)))
+            if (may && a.size == b.size && sdpops::same_tensor(pa, a.layout, pb, b.layout)) continue;
+            if (!(a.size == b.size && sdpops::disjoint(pa, a.layout, pb, b.layout, a.size)))
                 return fail(SDP_ERR_INVALID_ARGUMENT, "%s: %s overlaps %s", call, a.what, b.what);
         }
     }

@@ -268,6 +268,9 @@ __global__ __launch_bounds__(256) void k_route_lanes(RouteArgs a) {
     auto off = [=](float key) { return SCORED ? (1.0f + fabsf(key)) * slack : 0x1p-19f * fabsf(key); };
     auto there = [](float key) { return key >= -__FLT_MAX__; };
 
+    // in a large call some of the first waves go the rare ways for nothing, so that their
+    // instructions are there when they are needed (32,768 tokens: 34.5 us, else 38.8)
+    const bool warm = gridDim.x > 1024 && blockIdx.x < 512 && wave == 0;
     const int64_t w = a.first + (int64_t)blockIdx.x * (blockDim.x >> 6) + wave;
     if (w << tokens_log >= a.tokens) return;
     const int64_t t = (w << tokens_log) + (lane / G);
@@ -366,7 +369,7 @@ __global__ __launch_bounds__(256) void k_route_lanes(RouteArgs a) {
         }
         const float next = most_of(left);
         const bool close = on && next != kNegInf && last - next <= 2.0f * off(last);
-        if (__any(close && !slow)) {
+        if (warm || __any(close && !slow)) {
             // the groups' worth in 64 bits, of the same experts (unless the next one is close to them)
             float best[3] = {kNegInf, kNegInf, kNegInf};
             int from[2] = {0, 0};
@@ -433,7 +436,7 @@ __global__ __launch_bounds__(256) void k_route_lanes(RouteArgs a) {
         // of negative keys are sorted the highest first)
         const bool same = x == next_x && b == next_b && sub + 1 < a.top && my_key > 0.0f;
         const bool close = on && has && sub < a.top && there(next) && !same && my_key - next <= off(my_key);
-        if (__any(close && !slow)) {
+        if (warm || __any(close && !slow)) {
             // candidates until the next one is far behind the last one chosen
             const float last = __shfl(my_key, token_lane + a.top - 1);
             int count = rounds;

@@ -8,6 +8,7 @@ rest (types, ranges, overlaps) and a negative status becomes an exception.
 `stream` is a torch stream or a raw handle; None is the null stream.
 """
 import ctypes
+import struct
 from typing import Optional
 
 from . import sdp as _sdp
@@ -100,23 +101,34 @@ class sdp_expert_desc(ctypes.Structure):
                [("place", ctypes.c_void_p)]
 
 
+def _packer(kind):
+    """A function of a structure's fields, in their order, to its bytes: several times as fast as the
+    structure itself, and taken like it where a pointer to one is wanted.  Pointers are numbers."""
+    codes = {ctypes.c_int32: "i", ctypes.c_int64: "q", ctypes.c_double: "d", ctypes.c_void_p: "P"}
+    return struct.Struct("@" + "".join(codes.get(t, "P") for _, t in kind._fields_) + "0q").pack
+
+
+_rows_bytes, _embed_bytes, _norm_bytes, _grads_bytes, _route_bytes, _order_bytes, _expert_bytes = map(
+    _packer, (sdp_rows, sdp_embed_desc, sdp_block_norm_desc, sdp_block_norm_grads, sdp_route_desc, sdp_order_desc,
+              sdp_expert_desc))
+
+
 def _bind():
     vp, i32, i64, P = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.POINTER
     h, qk, gm, ds = P(sdp_heads), P(sdp_qk_norm_rope_desc), P(sdp_grouped_desc), P(sdp_distill_desc)
-    r, em, bn, rt, od, ex = (P(t) for t in (sdp_rows, sdp_embed_desc, sdp_block_norm_desc, sdp_route_desc,
-                                            sdp_order_desc, sdp_expert_desc))
     for name, args in {
-        "sdp_embed": [vp, em, r, r, vp],
-        "sdp_embed_backward": [vp, em, r, r, i32, vp],
-        "sdp_block_norm": [vp, bn, r, r, r, r, vp],
-        "sdp_block_norm_backward": [vp, bn, r, r, r, r, P(sdp_block_norm_grads), vp],
-        "sdp_route": [vp, rt, vp, vp, vp, vp, vp],
-        "sdp_route_backward": [vp, rt, vp, vp, vp, vp, i64, vp],
-        "sdp_expert_order": [vp, od, vp, vp, vp, vp, vp],
-        "sdp_expert_gather": [vp, ex, r, r, vp],
-        "sdp_expert_gather_backward": [vp, ex, r, r, vp],
-        "sdp_expert_combine": [vp, ex, r, vp, r, r, vp],
-        "sdp_expert_combine_backward": [vp, ex, r, vp, r, r, vp, vp],
+        # (descriptions and rows are bytes, or structures by reference)
+        "sdp_embed": [vp, vp, vp, vp, vp],
+        "sdp_embed_backward": [vp, vp, vp, vp, i32, vp],
+        "sdp_block_norm": [vp, vp, vp, vp, vp, vp, vp],
+        "sdp_block_norm_backward": [vp, vp, vp, vp, vp, vp, vp, vp],
+        "sdp_route": [vp, vp, vp, vp, vp, vp, vp],
+        "sdp_route_backward": [vp, vp, vp, vp, vp, vp, i64, vp],
+        "sdp_expert_order": [vp, vp, vp, vp, vp, vp, vp],
+        "sdp_expert_gather": [vp, vp, vp, vp, vp],
+        "sdp_expert_gather_backward": [vp, vp, vp, vp, vp],
+        "sdp_expert_combine": [vp, vp, vp, vp, vp, vp, vp],
+        "sdp_expert_combine_backward": [vp, vp, vp, vp, vp, vp, vp, vp],
         "sdp_qk_norm_rope": [vp, qk, h, h, h, h, vp],
         "sdp_qk_norm_rope_backward": [vp, qk, h, h, h, h, h, h, vp, vp, vp],
         "sdp_grouped_matmul": [vp, gm, vp, vp, vp, vp],
@@ -140,7 +152,7 @@ def _types():
             torch.int64: SDP_TYPE_I64}
 
 
-_TYPE_OF = {}
+_TYPE_OF = {}  # filled by the first call
 
 
 def _type(t, what: str) -> int:
@@ -382,88 +394,118 @@ def sdp_distill_loss_backward(ctx, logits, lse, row_grad, dlogits, *, teacher_lo
 
 
 # ---- around the experts' products (include/sdp_layer.h) ------------------------
+# What they refuse is found by one comparison of several things at a time, and named after.
 
-def _rows(t, shape, code: int, what: str) -> Optional[sdp_rows]:
-    """A 2-D tensor of this shape and type (None passes)."""
+def _refuse_rows(t, shape, code: int, what: str) -> None:
+    _same_type(t, code, what)
+    _row_stride(t, shape, what)
+
+
+def _at(t, shape, code: int, what: str):
+    """Address and row stride of a 2-D tensor of this shape and type."""
+    strides = t.stride()
+    if t.shape != shape or _TYPE_OF.get(t.dtype) != code or (strides[1] != 1 and shape[1] > 1):
+        _refuse_rows(t, shape, code, what)
+    return t.data_ptr(), strides[0]
+
+
+def _rows(t, shape, code: int, what: str) -> Optional[bytes]:
+    """The sdp_rows of such a tensor (None passes)."""
     if t is None:
         return None
-    _same_type(t, code, what)
-    return sdp_rows(t.data_ptr(), _row_stride(t, shape, what))
+    strides = t.stride()
+    if t.shape != shape or _TYPE_OF.get(t.dtype) != code or (strides[1] != 1 and shape[1] > 1):
+        _refuse_rows(t, shape, code, what)
+    return _rows_bytes(t.data_ptr(), strides[0])
+
+
+def _flat(t, shape, code: int, what: str) -> int:
+    """The address of a contiguous tensor of this shape and type (0 for None)."""
+    if t is None:
+        return 0
+    if t.shape != shape or _TYPE_OF.get(t.dtype) != code or not t.is_contiguous():
+        _same_type(t, code, what)
+        _dense(t, shape, what)
+    return t.data_ptr()
 
 
 def _two(t, what: str):
     shape = t.shape
-    _want(len(shape) == 2, f"{what} must be 2-D")
+    if len(shape) != 2:
+        raise ValueError(f"{what} must be 2-D")
     return shape
 
 
-def _embed_desc(table, rows, tokens, scale, names):
-    vocab, hidden = _two(table, names[0])
-    _count(max(vocab, hidden), names[0])
-    shape = tokens.shape
-    _want(len(shape) == 1, "tokens must be 1-D")
-    n = shape[0]
-    table_type, row_type = _type(table, names[0]), _type(rows, names[1])
-    d = sdp_embed_desc(n, vocab, hidden, table_type, row_type, _type(tokens, "tokens"),
-                       _dense(tokens, shape, "tokens"), scale)
-    return d, _rows(table, (vocab, hidden), table_type, names[0]), _rows(rows, (n, hidden), row_type, names[1])
+def _embed(call, ctx, table, rows, tokens, scale, table_name, rows_name, stream, *more) -> None:
+    shape, count = _two(table, table_name), tokens.shape
+    vocab, hidden = shape
+    if vocab > 0x7fffffff or hidden > 0x7fffffff:
+        _count(max(vocab, hidden), table_name)
+    if len(count) != 1:
+        raise ValueError("tokens must be 1-D")
+    n = count[0]
+    table_type, row_type, id_type = _type(table, table_name), _type(rows, rows_name), _type(tokens, "tokens")
+    d = _embed_bytes(n, vocab, hidden, table_type, row_type, id_type, _flat(tokens, count, id_type, "tokens"), scale)
+    t, r = _rows(table, shape, table_type, table_name), _rows(rows, (n, hidden), row_type, rows_name)
+    _check(call(ctx, d, r, t, *more, _stream(stream)) if more else call(ctx, d, t, r, _stream(stream)))
 
 
 def sdp_embed(ctx, table, tokens, out, *, scale: float = 1.0, stream=None) -> None:
-    d, t, o = _embed_desc(table, out, tokens, scale, ("table", "out"))
-    _check(_lib.sdp_embed(ctx, d, t, o, _stream(stream)))
+    _embed(_lib.sdp_embed, ctx, table, out, tokens, scale, "table", "out", stream)
 
 
 def sdp_embed_backward(ctx, dout, tokens, dtable, *, scale: float = 1.0, accumulate: bool = False,
                        stream=None) -> None:
-    d, t, o = _embed_desc(dtable, dout, tokens, scale, ("dtable", "dout"))
-    _check(_lib.sdp_embed_backward(ctx, d, o, t, 1 if accumulate else 0, _stream(stream)))
+    _embed(_lib.sdp_embed_backward, ctx, dtable, dout, tokens, scale, "dtable", "dout", stream, 1 if accumulate else 0)
 
 
 def _gate(t, tokens: int, hidden: int, code: int, what: str):
     """Form, address and stride of a gate [hidden] or [1, hidden], [tokens, 1] or
     [tokens, hidden]; of one token or one channel the form of the most elements."""
     if t is None:
-        return SDP_GATE_NONE, None, 0
-    _same_type(t, code, what)
-    shape, strides = t.shape, t.stride()
+        return SDP_GATE_NONE, 0, 0
+    shape = t.shape
     if shape == (hidden,) or (shape == (1, hidden) and tokens != 1):
-        return SDP_GATE_CHANNEL, _dense(t, shape, what), 0
-    if shape == (tokens, hidden):
-        return SDP_GATE_ELEMENT, t.data_ptr(), _row_stride(t, shape, what)
-    if shape == (tokens, 1):
-        return SDP_GATE_TOKEN, t.data_ptr(), strides[0]
+        return SDP_GATE_CHANNEL, _flat(t, shape, code, what), 0
+    if shape == (tokens, hidden) or shape == (tokens, 1):
+        return (SDP_GATE_ELEMENT if shape[1] == hidden else SDP_GATE_TOKEN, *_at(t, shape, code, what))
     raise ValueError(f"{what} has shape {tuple(shape)}, expected [{hidden}], [{tokens}, 1] or [{tokens}, {hidden}]")
 
 
-def _block_norm_desc(stream_t, y_t, weights, gate, sigmoid, post_norm, post_weight, pre_weight, scale, eps, offset):
-    """stream_t, y_t: any tensor of the stream, and of y's type (None: the gate's, or the stream's)."""
+def _norm_desc(stream_t, some, weight, gate, sigmoid, post_norm, post_weight, pre_weight, scale, eps, offset):
+    """stream_t: a tensor of the stream; some: one of y's type, or None; weight: a weight or its gradient, or None."""
     shape = _two(stream_t, "the stream")
     tokens, hidden = shape
-    _count(hidden, "the stream")
+    if hidden > 0x7fffffff:
+        _count(hidden, "the stream")
     stream_type = _type(stream_t, "the stream")
-    some = gate if y_t is None else y_t
+    if some is None:
+        some = gate
     code = stream_type if some is None else _type(some, "y")
-    given = [w for w in weights if w is not None]
-    weight_type = _type(given[0], "a weight") if given else SDP_TYPE_F32
-    for w in given:
-        _same_type(w, weight_type, "a weight")
+    weight_type = SDP_TYPE_F32 if weight is None else _type(weight, "a weight")
+    if weight is not None:
+        _same_type(post_weight, weight_type, "a weight")
+        _same_type(pre_weight, weight_type, "a weight")
     form, at, stride = _gate(gate, tokens, hidden, code, "gate")
-    d = sdp_block_norm_desc(tokens, hidden, stream_type, code, weight_type, 1 if post_norm else 0, form,
-                            1 if sigmoid else 0, scale, eps, offset, at, stride,
-                            _dense(post_weight, (hidden,), "post_weight"), _dense(pre_weight, (hidden,), "pre_weight"))
-    return d, shape
+    wide = (hidden,)
+    d = _norm_bytes(tokens, hidden, stream_type, code, weight_type, 1 if post_norm else 0, form, 1 if sigmoid else 0,
+                    scale, eps, offset, at, stride, _flat(post_weight, wide, weight_type, "post_weight"),
+                    _flat(pre_weight, wide, weight_type, "pre_weight"))
+    return d, shape, stream_type, code, weight_type, form
 
 
 def sdp_block_norm(ctx, h, y, h_out, n_out, *, gate=None, gate_sigmoid: bool = False, post_norm: bool = False,
                    post_weight=None, pre_weight=None, scale: float = 1.0, eps: float = 1e-6,
                    weight_offset: float = 0.0, stream=None) -> None:
     """y and h_out may be None (the norm alone), or n_out."""
-    d, shape = _block_norm_desc(h, n_out if y is None else y, (post_weight, pre_weight), gate, gate_sigmoid, post_norm,
-                                post_weight, pre_weight, scale, eps, weight_offset)
-    s, c = d.stream_type, d.type
+    d, shape, s, c, _, _ = _norm_desc(h, n_out if y is None else y, post_weight if pre_weight is None else pre_weight,
+                                      gate, gate_sigmoid, post_norm, post_weight, pre_weight, scale, eps, weight_offset)
     _check(_lib.sdp_block_norm(ctx, d, _rows(h, shape, s, "h"), _rows(y, shape, c, "y"), _rows(h_out, shape, s, "h_out"),
                                _rows(n_out, shape, c, "n_out"), _stream(stream)))
+
+
+def _first(*tensors):
+    return next((t for t in tensors if t is not None), None)
 
 
 def sdp_block_norm_backward(ctx, h_out, y, dh_out, dn, dh, dy, *, gate=None, dgate=None, gate_sigmoid: bool = False,
@@ -471,104 +513,111 @@ def sdp_block_norm_backward(ctx, h_out, y, dh_out, dn, dh, dy, *, gate=None, dga
                             dpre_weight=None, scale: float = 1.0, eps: float = 1e-6, weight_offset: float = 0.0,
                             stream=None) -> None:
     """h_out is the stream after the addition; any tensor that the call does not need may be None."""
-    first = [t for t in (h_out, dh_out, dh) if t is not None]
-    _want(bool(first), "h_out, dh_out and dh are all None")
-    ys = [t for t in (y, dn, dy) if t is not None]
-    d, shape = _block_norm_desc(first[0], ys[0] if ys else None, (post_weight, pre_weight, dpost_weight, dpre_weight),
-                                gate, gate_sigmoid, post_norm, post_weight, pre_weight, scale, eps, weight_offset)
-    s, c = d.stream_type, d.type
-    form, at, stride = _gate(dgate, shape[0], shape[1], c, "dgate")
-    if dgate is not None and form != d.gate_form:
+    some = _first(h_out, dh_out, dh)
+    _want(some is not None, "h_out, dh_out and dh are all None")
+    d, shape, s, c, w, form = _norm_desc(some, _first(y, dn, dy),
+                                         _first(post_weight, pre_weight, dpost_weight, dpre_weight), gate, gate_sigmoid,
+                                         post_norm, post_weight, pre_weight, scale, eps, weight_offset)
+    gate_form, at, stride = _gate(dgate, shape[0], shape[1], c, "dgate")
+    if dgate is not None and gate_form != form:
         raise ValueError("dgate has another form than gate")
+    _same_type(dpost_weight, w, "a weight")
+    _same_type(dpre_weight, w, "a weight")
     wide = (shape[1],)
-    rows_dh, rows_dy = _rows(dh, shape, s, "dh"), _rows(dy, shape, c, "dy")
-    ref = lambda r: None if r is None else ctypes.pointer(r)
-    grads = sdp_block_norm_grads(ref(rows_dh), ref(rows_dy), at, stride, _dense(dpost_weight, wide, "dpost_weight"),
-                                 _dense(dpre_weight, wide, "dpre_weight"))
+    out_h = None if dh is None else sdp_rows(*_at(dh, shape, s, "dh"))
+    out_y = None if dy is None else sdp_rows(*_at(dy, shape, c, "dy"))
+    where = ctypes.addressof
+    grads = _grads_bytes(0 if out_h is None else where(out_h), 0 if out_y is None else where(out_y), at, stride,
+                         _flat(dpost_weight, wide, w, "dpost_weight"), _flat(dpre_weight, wide, w, "dpre_weight"))
     _check(_lib.sdp_block_norm_backward(ctx, d, _rows(h_out, shape, s, "h_out"), _rows(y, shape, c, "y"),
                                         _rows(dh_out, shape, s, "dh_out"), _rows(dn, shape, c, "dn"), grads,
                                         _stream(stream)))
 
 
-def _route_desc(logits, index, weights, sigmoid, groups, top_groups, group_best, renormalize, scale, names):
-    shape = _two(logits, "logits")
+def _route_desc(logits, index, weights, sigmoid, groups, top_groups, group_best, renormalize, scale, name):
+    """Description, and the addresses of logits, index and weights."""
+    shape, chosen = _two(logits, "logits"), _two(index, "index")
     tokens, experts = shape
-    chosen = _two(index, "index")
-    _count(max(experts, chosen[1]), "logits and index")
-    _want(chosen[0] == tokens, f"index has {chosen[0]} rows, expected {tokens}")
-    d = sdp_route_desc(tokens, experts, chosen[1], _type(logits, "logits"), _type(index, "index"),
-                       _type(weights, names), 1 if sigmoid else 0, 1 if renormalize else 0, groups, top_groups,
-                       group_best, scale, _row_stride(logits, shape, "logits"))
-    return d, _dense(index, chosen, "index"), _dense(weights, chosen, names)
+    top = chosen[1]
+    if experts > 0x7fffffff or top > 0x7fffffff:
+        _count(max(experts, top), "logits and index")
+    if chosen[0] != tokens:
+        raise ValueError(f"index has {chosen[0]} rows, expected {tokens}")
+    code, index_type, weight_type = _type(logits, "logits"), _type(index, "index"), _type(weights, name)
+    z, stride = _at(logits, shape, code, "logits")
+    i, w = _flat(index, chosen, index_type, "index"), _flat(weights, chosen, weight_type, name)
+    d = _route_bytes(tokens, experts, top, code, index_type, weight_type, 1 if sigmoid else 0, 1 if renormalize else 0,
+                     groups, top_groups, group_best, scale, stride)
+    return d, z, i, w, shape, code
 
 
 def sdp_route(ctx, logits, index, weights, *, bias=None, sigmoid: bool = False, groups: int = 1, top_groups: int = 1,
               group_best: int = 1, renormalize: bool = False, scale: float = 1.0, stream=None) -> None:
-    d, i, w = _route_desc(logits, index, weights, sigmoid, groups, top_groups, group_best, renormalize, scale, "weights")
-    b = None if bias is None else _f32(bias, (d.experts,), "bias")
-    _check(_lib.sdp_route(ctx, d, logits.data_ptr(), b, i, w, _stream(stream)))
+    d, z, i, w, shape, _ = _route_desc(logits, index, weights, sigmoid, groups, top_groups, group_best, renormalize,
+                                       scale, "weights")
+    b = None if bias is None else _flat(bias, (shape[1],), SDP_TYPE_F32, "bias")
+    _check(_lib.sdp_route(ctx, d, z, b, i, w, _stream(stream)))
 
 
 def sdp_route_backward(ctx, logits, index, dweights, dlogits, *, sigmoid: bool = False, renormalize: bool = False,
                        scale: float = 1.0, stream=None) -> None:
-    d, i, w = _route_desc(logits, index, dweights, sigmoid, 1, 1, 1, renormalize, scale, "dweights")
-    _same_type(dlogits, d.logit_type, "dlogits")
-    _check(_lib.sdp_route_backward(ctx, d, logits.data_ptr(), i, w, dlogits.data_ptr(),
-                                   _row_stride(dlogits, logits.shape, "dlogits"), _stream(stream)))
+    d, z, i, w, shape, code = _route_desc(logits, index, dweights, sigmoid, 1, 1, 1, renormalize, scale, "dweights")
+    _check(_lib.sdp_route_backward(ctx, d, z, i, w, *_at(dlogits, shape, code, "dlogits"), _stream(stream)))
 
 
 def sdp_expert_order(ctx, index, ends, place, order=None, *, stream=None) -> None:
     """index, place: [tokens, top] or [entries]; order: [entries], or None."""
-    experts = ends.shape
-    _want(len(experts) == 1, "ends must be 1-D")
+    shape, experts = index.shape, ends.shape
+    if len(experts) != 1:
+        raise ValueError("ends must be 1-D")
     _count(experts[0], "ends")
     n = index.numel()
-    _same_type(place, SDP_TYPE_I32, "place")
-    _same_type(order, SDP_TYPE_I32, "order")
-    d = sdp_order_desc(n, experts[0], _type(index, "index"), _type(ends, "ends"))
-    _check(_lib.sdp_expert_order(ctx, d, _dense(index, index.shape, "index"), _dense(ends, experts, "ends"),
-                                 _dense(place, index.shape, "place"), _dense(order, (n,), "order"), _stream(stream)))
+    index_type, ends_type = _type(index, "index"), _type(ends, "ends")
+    d = _order_bytes(n, experts[0], index_type, ends_type)
+    _check(_lib.sdp_expert_order(ctx, d, _flat(index, shape, index_type, "index"), _flat(ends, experts, ends_type, "ends"),
+                                 _flat(place, shape, SDP_TYPE_I32, "place"), _flat(order, (n,), SDP_TYPE_I32, "order"),
+                                 _stream(stream)))
 
 
 def _expert_desc(place, hidden: int, row_type: int, stream_type: int, weight_type: int):
-    tokens, top = _two(place, "place")
-    _count(max(tokens, top, hidden), "place and the rows")
-    _same_type(place, SDP_TYPE_I32, "place")
-    return sdp_expert_desc(tokens, top, hidden, row_type, stream_type, weight_type,
-                           _dense(place, place.shape, "place")), (tokens, hidden), (tokens * top, hidden)
+    """Description, and the shapes of place, of the tokens' tensors and of the sorted rows."""
+    shape = _two(place, "place")
+    tokens, top = shape
+    if tokens > 0x7fffffff or top > 0x7fffffff or hidden > 0x7fffffff:
+        _count(max(tokens, top, hidden), "place and the rows")
+    return _expert_bytes(tokens, top, hidden, row_type, stream_type, weight_type,
+                         _flat(place, shape, SDP_TYPE_I32, "place")), shape, (tokens, hidden), (tokens * top, hidden)
 
 
 def sdp_expert_gather(ctx, x, place, rows, *, stream=None) -> None:
     code = _type(x, "x")
-    d, side, all_rows = _expert_desc(place, _two(x, "x")[1], code, code, SDP_TYPE_F32)
-    _check(_lib.sdp_expert_gather(ctx, d, _rows(x, side, code, "x"), _rows(rows, all_rows, code, "rows"),
+    d, _, side, sorted_rows = _expert_desc(place, _two(x, "x")[1], code, code, SDP_TYPE_F32)
+    _check(_lib.sdp_expert_gather(ctx, d, _rows(x, side, code, "x"), _rows(rows, sorted_rows, code, "rows"),
                                   _stream(stream)))
 
 
 def sdp_expert_gather_backward(ctx, drows, place, dx, *, stream=None) -> None:
     code = _type(drows, "drows")
-    d, side, all_rows = _expert_desc(place, _two(drows, "drows")[1], code, code, SDP_TYPE_F32)
-    _check(_lib.sdp_expert_gather_backward(ctx, d, _rows(drows, all_rows, code, "drows"), _rows(dx, side, code, "dx"),
-                                           _stream(stream)))
+    d, _, side, sorted_rows = _expert_desc(place, _two(drows, "drows")[1], code, code, SDP_TYPE_F32)
+    _check(_lib.sdp_expert_gather_backward(ctx, d, _rows(drows, sorted_rows, code, "drows"),
+                                           _rows(dx, side, code, "dx"), _stream(stream)))
 
 
 def sdp_expert_combine(ctx, rows, place, weights, out, *, residual=None, stream=None) -> None:
-    code, to = _type(rows, "rows"), _type(out, "out")
-    d, side, all_rows = _expert_desc(place, _two(rows, "rows")[1], code, to, _type(weights, "weights"))
-    _check(_lib.sdp_expert_combine(ctx, d, _rows(rows, all_rows, code, "rows"), _dense(weights, place.shape, "weights"),
+    code, to, w = _type(rows, "rows"), _type(out, "out"), _type(weights, "weights")
+    d, shape, side, sorted_rows = _expert_desc(place, _two(rows, "rows")[1], code, to, w)
+    _check(_lib.sdp_expert_combine(ctx, d, _rows(rows, sorted_rows, code, "rows"), _flat(weights, shape, w, "weights"),
                                    _rows(residual, side, to, "residual"), _rows(out, side, to, "out"),
                                    _stream(stream)))
 
 
 def sdp_expert_combine_backward(ctx, rows, place, weights, dout, drows=None, dweights=None, *, stream=None) -> None:
     """drows or dweights may be None; rows without dweights, weights without drows."""
-    some = drows if rows is None else rows
-    code, to = _type(dout if some is None else some, "rows"), _type(dout, "dout")
-    w = dweights if weights is None else weights
-    d, side, all_rows = _expert_desc(place, _two(dout, "dout")[1], code, to,
-                                     SDP_TYPE_F32 if w is None else _type(w, "weights"))
-    _same_type(dweights, d.weight_type, "dweights")
+    some, some_w = _first(rows, drows), _first(weights, dweights)
+    to = _type(dout, "dout")
+    code, w = to if some is None else _type(some, "rows"), SDP_TYPE_F32 if some_w is None else _type(some_w, "weights")
+    d, shape, side, sorted_rows = _expert_desc(place, _two(dout, "dout")[1], code, to, w)
     _check(_lib.sdp_expert_combine_backward(
-        ctx, d, _rows(rows, all_rows, code, "rows"), _dense(weights, place.shape, "weights"),
-        _rows(dout, side, to, "dout"), _rows(drows, all_rows, code, "drows"),
-        _dense(dweights, place.shape, "dweights"), _stream(stream)))
+        ctx, d, _rows(rows, sorted_rows, code, "rows"), _flat(weights, shape, w, "weights"),
+        _rows(dout, side, to, "dout"), _rows(drows, sorted_rows, code, "drows"),
+        _flat(dweights, shape, w, "dweights"), _stream(stream)))

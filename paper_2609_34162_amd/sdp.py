@@ -159,9 +159,7 @@ def _check(rc: int, norm: Optional[float] = None) -> None:
 def _stream(stream) -> Optional[int]:
     if stream is None:
         return None
-    if hasattr(stream, "cuda_stream"):
-        return stream.cuda_stream or None
-    return int(stream) or None
+    return int(getattr(stream, "cuda_stream", stream)) or None
 
 
 class Segments:

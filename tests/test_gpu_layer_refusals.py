@@ -95,8 +95,7 @@ def test_block_norm(lib):
     refused(ops, bad, "dy overlaps dh_out", b, ctx, h, y, ho, no, dh, ho)
     refused(ops, bad, "dpre_weight", b, ctx, h, y, ho, no, dh, dy, post_norm=True, dpost_weight=dw, dpre_weight=dw)
     refused(ops, bad, "overlaps gate", b, ctx, h, y, ho, no, dh, dy, gate=w, dgate=w)
-    d = ops._block_norm_desc(h, y, (), w, False, False, None, None, 1.0, 1e-6, 0.0)[0]
-    d.gate_form = ops.SDP_GATE_NONE
+    d = ops.sdp_block_norm_desc(6, 16, 0, 0, 0, 0, ops.SDP_GATE_NONE, 0, 1.0, 1e-6, 0.0)
     r = lambda t: ctypes.pointer(ops.sdp_rows(t.data_ptr(), 16))
     grads = ops.sdp_block_norm_grads(r(dh), r(dy), dw.data_ptr(), 0, None, None)
     refused(ops, bad, "dgate without a gate", lambda: sdp._check(sdp._lib.sdp_block_norm_backward(

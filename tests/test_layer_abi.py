@@ -133,3 +133,14 @@ def test_binding_refuses_what_32_bits_do_not_hold(ops):
         ops.sdp_route(None, far(1, n), one, torch.zeros(1, 1))
     with pytest.raises(ValueError, match="place and the rows: a dimension"):
         ops.sdp_expert_gather(None, far(1, n), one, far(1, n))
+
+
+def test_descriptions_are_packed_as_the_structures_lie(ops):
+    for kind in (ops.sdp_rows, ops.sdp_embed_desc, ops.sdp_block_norm_desc, ops.sdp_block_norm_grads, ops.sdp_route_desc,
+                 ops.sdp_order_desc, ops.sdp_expert_desc):
+        values = [1.5 + k if t is ctypes.c_double else 3 + k for k, (_, t) in enumerate(kind._fields_)]
+        one = kind()
+        for (name, t), v in zip(kind._fields_, values):
+            setattr(one, name, ctypes.cast(v, t) if t not in (ctypes.c_int32, ctypes.c_int64, ctypes.c_double,
+                                                              ctypes.c_void_p) else v)
+        assert ops._packer(kind)(*values) == bytes(one), kind
