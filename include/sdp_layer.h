@@ -71,7 +71,7 @@ SDP_API int sdp_embed(sdp_ctx *ctx, const sdp_embed_desc *desc, const sdp_rows *
                       void *stream);
 
 /* Its backward: dtable[v] = scale * the sum of dout[t] over the tokens with
- * ids[t] = v, in the tokens' order (in runs of 64 where there are many).
+ * ids[t] = v, in the tokens' order, 16 at a time.
  * accumulate 0: every row of dtable is written, those that no token names
  * with zeros; else the sum is added to what dtable holds (a table that is the
  * head's weight too), and rows that no token names are left as they are.

@@ -37,6 +37,7 @@ struct SortArgs {
     int32_t ends64;
     int32_t *keys_out;        // key at each place after the pass (may be NULL)
     int32_t *counts;          // [blocks] rows, counts_stride apart
+    bool apart;               // they are not place itself
     int64_t counts_stride;
     int64_t chunk;            // entries of a block
     int32_t blocks;
@@ -60,12 +61,10 @@ struct EmbedArgs {
     int32_t accumulate;
     // workspace of the gradient
     int32_t *order, *order_spare, *key, *key_spare, *counts;
-    // [pieces, 2, hidden] sums of what a piece of kEmbedPiece places has of ids that go on
+    // [pieces, 2, hidden] sums of what a piece of the places has of ids that go on
     // before it (or all through it) and of ids that go on behind it
     float *sums;
 };
-
-constexpr int kEmbedPiece = 64;
 
 size_t embed_workspace(EmbedArgs &a, char *space);
 hipError_t launch_embed(const EmbedArgs &a, bool table_bf16, bool rows_bf16, hipStream_t s);

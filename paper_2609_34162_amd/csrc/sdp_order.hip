@@ -13,7 +13,7 @@
 //  - three launches, for more entries: each block's counts, their running sums by one
 //    block, the places (13.8 us; 524,288 entries of 256 experts 28).  The counts of a
 //    block lie where its places will (or in a workspace), so that the call needs no
-//    memory of its own.
+//    memory of its own; where they lie apart, the second launch is part of the third.
 #include <algorithm>
 
 #include "sdp_layer_internal.h"
@@ -308,12 +308,39 @@ __global__ __launch_bounds__(64 * WAVES) void k_sort_scan(SortArgs a) {
     }
 }
 
-template <int WAVES>
+// SCANS: the counts are still the blocks' own, and each block adds up what it needs of them.
+template <int WAVES, bool SCANS>
 __global__ __launch_bounds__(64 * WAVES) void k_sort_place(SortArgs a) {
-    constexpr int kThreads = 64 * WAVES;
+    constexpr int kThreads = 64 * WAVES, kAhead = 8;
+    __shared__ int32_t wave_sums[WAVES];
     const Shared s = shared_of(a.digits);
-    // all of the block's row is read before any of its places is written over it
-    for (int d = threadIdx.x; d < a.digits; d += kThreads) s.base[d] = a.counts[blockIdx.x * a.counts_stride + d];
+    const int32_t *const mine = a.counts + (int64_t)blockIdx.x * a.counts_stride;
+    if (SCANS) {
+        for (int d = threadIdx.x; d < a.digits; d += kThreads) {
+            int32_t before = 0, all = 0;
+            for (int b = 0; b < a.blocks; b += kAhead) {
+                int32_t c[kAhead];
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u)
+                    c[u] = b + u < a.blocks ? a.counts[(b + u) * a.counts_stride + d] : 0;
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) {
+                    all += c[u];
+                    before += b + u < (int)blockIdx.x ? c[u] : 0;
+                }
+            }
+            s.total[d] = all, s.before[d] = before;
+        }
+        __syncthreads();
+        scan_digits(s.total, s.base, a.digits, wave_sums);
+        for (int d = threadIdx.x; d < a.digits; d += kThreads) {
+            if (blockIdx.x == 0) put_end(a, d, s.base[d] + s.total[d]);
+            s.base[d] += s.before[d];
+        }
+    } else {
+        // all of the block's row is read before any of its places is written over it
+        for (int d = threadIdx.x; d < a.digits; d += kThreads) s.base[d] = mine[d];
+    }
     __syncthreads();
     place_range<WAVES>(a, range_of(a), s);
 }
@@ -377,7 +404,10 @@ void sort_split(SortArgs &a) {
     a.blocks = (int32_t)std::max<int64_t>(1, a.n / chunk);  // the last one has the rest
 }
 
-bool sort_needs_counts(const SortArgs &a) { return a.n > most_counted_by_all(a); }
+// Up to how many blocks of entries each adds up the counts itself, where they lie apart.
+constexpr int kMostScannedByAll = 64;
+
+bool sort_needs_counts(const SortArgs &a) { return a.apart ? a.blocks > 1 : a.n > most_counted_by_all(a); }
 
 hipError_t launch_sort(const SortArgs &a, hipStream_t s) {
     auto go = [&](auto kernel, int blocks, int waves) {
@@ -398,12 +428,18 @@ hipError_t launch_sort(const SortArgs &a, hipStream_t s) {
     }
     constexpr int kScanWaves = 4;  // where there are many digits
     many ? go(k_sort_count<kManyWaves>, a.blocks, kManyWaves) : go(k_sort_count<kFewWaves>, a.blocks, kFewWaves);
+    if (a.apart && a.blocks <= kMostScannedByAll) {
+        many ? go(k_sort_place<kManyWaves, true>, a.blocks, kManyWaves)
+             : go(k_sort_place<kFewWaves, true>, a.blocks, kFewWaves);
+        return hipGetLastError();
+    }
     // (its sums have 32 bits, the steps' counts 16)
-    if (a.digits <= kMostScannedWide)
-        hipLaunchKernelGGL(k_sort_scan<kManyWaves>, dim3(1), dim3(64 * kManyWaves), shared_bytes(a.digits, 2 * kManyWaves), s, a);
-    else
-        hipLaunchKernelGGL(k_sort_scan<kScanWaves>, dim3(1), dim3(64 * kScanWaves), shared_bytes(a.digits, 2 * kScanWaves), s, a);
-    many ? go(k_sort_place<kManyWaves>, a.blocks, kManyWaves) : go(k_sort_place<kFewWaves>, a.blocks, kFewWaves);
+    auto scan = [&](auto kernel, int waves) {
+        hipLaunchKernelGGL(kernel, dim3(1), dim3(64 * waves), shared_bytes(a.digits, 2 * waves), s, a);
+    };
+    a.digits <= kMostScannedWide ? scan(k_sort_scan<kManyWaves>, kManyWaves) : scan(k_sort_scan<kScanWaves>, kScanWaves);
+    many ? go(k_sort_place<kManyWaves, false>, a.blocks, kManyWaves)
+         : go(k_sort_place<kFewWaves, false>, a.blocks, kFewWaves);
     return hipGetLastError();
 }
 

@@ -65,6 +65,24 @@ def test_runs_of_one_id(ctx, ids):
     check(ctx, torch.tensor(ids), 5, 40)
 
 
+@pytest.mark.parametrize("longest", [3, 20, 40, 130, 300])
+@pytest.mark.parametrize("row_type", [BF16, F32])
+def test_runs_across_waves_and_pieces(ctx, longest, row_type):
+    """Runs of every length, beginning and ending anywhere in a wave's places and a block's."""
+    gen = torch.Generator().manual_seed(longest)
+    lengths = torch.randint(1, longest + 1, (40,), generator=gen)
+    ids = torch.repeat_interleave(torch.arange(40) * 2, lengths)[torch.randperm(int(lengths.sum()), generator=gen)]
+    check(ctx, ids, 81, 520, row_type=row_type, seed=longest)
+
+
+@pytest.mark.parametrize("n", [30000, 131071, 133120, 300000])
+def test_many_tokens(ctx, n):
+    """The sort's ways for many entries, one pass and two."""
+    gen = torch.Generator().manual_seed(n)
+    for vocab in (900, 9000):
+        check(ctx, torch.randint(-1, vocab, (n,), generator=gen), vocab, 3, F32, F32)
+
+
 @pytest.mark.parametrize("vocab", [2047, 2048, 2049, 5000, 70000])
 def test_digits_of_ids(ctx, vocab):
     gen = torch.Generator().manual_seed(vocab)
