@@ -90,7 +90,7 @@ SDP_API int sdp_embed_backward(sdp_ctx *ctx, const sdp_embed_desc *desc, const s
  * and their gradients; type likewise, of the block's output y, n_out, the gate
  * and their gradients; weight_type likewise, of post_weight and pre_weight
  * ([hidden]; NULL: a factor of one) and their gradients.  A weight w counts as
- * weight_offset + w. */
+ * weight_offset + w.  tokens is at most 2^31 - 1. */
 typedef struct {
     int64_t tokens;
     int32_t hidden;

@@ -188,7 +188,8 @@ __global__ __launch_bounds__(kTableThreads) void k_embed_table(EmbedArgs a) {
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u)
                     // in its first piece the run comes last
-                    load_floats(a.sums + (2 * (int64_t)min(r + u, r1) + (r + u == r0 ? 1 : 0)) * a.hidden + c, left, x[u]);
+                    load_floats(a.sums + (2 * (int64_t)min(r + u, r1) + (r + u == r0 ? 1 : 0)) * a.hidden + c, left,
+                                x[u]);
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u)
 #pragma unroll

@@ -165,7 +165,9 @@ hipError_t launch_combine(const ExpertArgs &a, bool row_bf16, bool stream_bf16, 
     const int slices = a.hidden / kColumns + (a.hidden % kColumns != 0);
     const int64_t waves = a.tokens * slices;
     if (waves == 0) return hipSuccess;
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(grid_of(waves)), dim3(64 * kWaves), 0, s, a, slices); };
+    auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3(grid_of(waves)), dim3(64 * kWaves), 0, s, a, slices);
+    };
     const bool once = past_cache(a.tokens * a.hidden * ((int64_t)a.top * (row_bf16 ? 2 : 4) + (stream_bf16 ? 4 : 8)));
     auto pick = [&](auto is_once) {
         constexpr bool O = decltype(is_once)::value;

@@ -19,7 +19,8 @@ int need(const char *call, const sdp_ctx *ctx, const void *desc) {
 Rows kernel_rows(const sdp_rows *r) { return r ? Rows{r->data, r->stride} : Rows{nullptr, 0}; }
 
 // Adds a [rows, cols] tensor to a call's; absent ones have no elements.
-int add(std::vector<Tensor> &ts, const char *what, const sdp_rows *r, int64_t rows, int64_t cols, int type, bool written) {
+int add(std::vector<Tensor> &ts, const char *what, const sdp_rows *r, int64_t rows, int64_t cols, int type,
+        bool written) {
     ts.push_back(rows_of(what, r ? r->data : nullptr, r ? rows : 0, r ? r->stride : 0, cols, type_size(type), written));
     return (int)ts.size() - 1;
 }
@@ -70,7 +71,7 @@ int embed_call(sdp_ctx *ctx, const char *call, const sdp_embed_desc *d, const sd
 
 int check_norm(const char *call, sdp_ctx *ctx, const sdp_block_norm_desc *d) {
     SDP_TRY(need(call, ctx, d));
-    if (d->tokens < 0 || d->hidden < 0)
+    if (d->tokens < 0 || d->tokens > INT32_MAX || d->hidden < 0)
         return fail(SDP_ERR_INVALID_ARGUMENT, "%s: tokens or hidden out of range", call);
     if (!is_float_type(d->stream_type) || !is_float_type(d->type) || !is_float_type(d->weight_type))
         return fail(SDP_ERR_INVALID_ARGUMENT, "%s: a type is none of those allowed", call);

@@ -437,7 +437,8 @@ hipError_t launch_sort(const SortArgs &a, hipStream_t s) {
     auto scan = [&](auto kernel, int waves) {
         hipLaunchKernelGGL(kernel, dim3(1), dim3(64 * waves), shared_bytes(a.digits, 2 * waves), s, a);
     };
-    a.digits <= kMostScannedWide ? scan(k_sort_scan<kManyWaves>, kManyWaves) : scan(k_sort_scan<kScanWaves>, kScanWaves);
+    a.digits <= kMostScannedWide ? scan(k_sort_scan<kManyWaves>, kManyWaves)
+                                 : scan(k_sort_scan<kScanWaves>, kScanWaves);
     many ? go(k_sort_place<kManyWaves, false>, a.blocks, kManyWaves)
          : go(k_sort_place<kFewWaves, false>, a.blocks, kFewWaves);
     return hipGetLastError();

@@ -670,7 +670,8 @@ hipError_t launch_route_any(const RouteArgs &args, hipStream_t s) {
     const Split split = split_of(a, a.top + (scored || sizeof(T) == 4));  // one more is looked at than is chosen
     const size_t space = (size_t)a.experts * 16;  // of a wave
     if (!split.lanes) {
-        hipLaunchKernelGGL((k_route_any<T>), dim3((uint32_t)std::min<int64_t>(a.tokens, 1 << 20)), dim3(64), space, s, a);
+        const dim3 grid((uint32_t)std::min<int64_t>(a.tokens, 1 << 20));
+        hipLaunchKernelGGL((k_route_any<T>), grid, dim3(64), space, s, a);
         return hipGetLastError();
     }
     a.lanes = split.lanes;
@@ -682,7 +683,8 @@ hipError_t launch_route_any(const RouteArgs &args, hipStream_t s) {
         constexpr int64_t kMost = 1 << 22;
         for (a.first = 0; a.first < items; a.first += kMost) {
             const int64_t n = std::min(kMost, items - a.first);
-            hipLaunchKernelGGL(kernel, dim3((uint32_t)((n + waves - 1) / waves)), dim3(64 * waves), space * waves, s, a);
+            const dim3 grid((uint32_t)((n + waves - 1) / waves));
+            hipLaunchKernelGGL(kernel, grid, dim3(64 * waves), space * waves, s, a);
         }
     };
     auto pick = [&](auto n) {
@@ -708,7 +710,8 @@ hipError_t launch_back_any(const RouteArgs &args, hipStream_t s) {
     a.groups = 1;
     const Split split = split_of(a, a.top);
     if (!split.lanes) {
-        hipLaunchKernelGGL((k_route_back_any<T>), dim3((uint32_t)std::min<int64_t>(a.tokens, 1 << 20)), dim3(64), 0, s, a);
+        const dim3 grid((uint32_t)std::min<int64_t>(a.tokens, 1 << 20));
+        hipLaunchKernelGGL((k_route_back_any<T>), grid, dim3(64), 0, s, a);
         return hipGetLastError();
     }
     a.lanes = split.lanes;
