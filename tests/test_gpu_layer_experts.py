@@ -132,7 +132,7 @@ def check_rows(ctx, t, k, experts, h, dtype=BF16, stream=BF16, wtype=F32, pad=0,
 
 
 @pytest.mark.parametrize("dtype,stream,wtype", [(BF16, BF16, F32), (F32, F32, F32), (BF16, F32, BF16), (F32, BF16, F32)])
-@pytest.mark.parametrize("h", [1, 7, 8, 9, 100, 512, 513, 1000, 1024, 2048, 5000])
+@pytest.mark.parametrize("h", [1, 7, 8, 9, 100, 120, 128, 129, 208, 256, 257, 512, 513, 550, 1000, 1024, 2048, 5000])
 def test_hidden_sizes_and_types(ctx, h, dtype, stream, wtype):
     check_rows(ctx, 37, 3, 5, h, dtype, stream, wtype, seed=h)
 
