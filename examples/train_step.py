@@ -1,15 +1,17 @@
 """A small training program around the update: a student with normed and rotated
 queries and keys and routed experts learns a teacher's top logits.
 
-One decoder layer: attention whose queries and keys go through
-sdp_qk_norm_rope, then a mixture of experts whose products are
-sdp_grouped_matmul (the tokens sorted by expert), then the head and
+One decoder layer: rows of the embedding (sdp_embed), attention whose queries
+and keys go through sdp_qk_norm_rope, then a mixture of experts: sdp_route
+chooses, sdp_expert_order sorts the entries by expert, sdp_expert_gather brings
+the tokens to their rows, the products are sdp_grouped_matmul, and
+sdp_expert_combine adds them up on the stream.  Then the head and
 sdp_distill_loss, which gives the loss and the logits' gradient in one call.
 The backward calls write BF16 gradients straight into the flat gradient buffer
-of an sdp_segment -- the experts' as they come from
-sdp_grouped_matmul_backward -- and sdp_agg_adam_step clips them, takes the step
-on the FP32 master weights and gives back the BF16 weights.  Attention's
-scores, the router and the dense products are plain torch.
+of an sdp_segment -- the embedding's and the experts' as they come -- and
+sdp_agg_adam_step clips them, takes the step on the FP32 master weights and
+gives back the BF16 weights.  Attention's scores and the dense products are
+plain torch.
 
     python3 examples/train_step.py [--steps 40]
 """
@@ -71,6 +73,82 @@ class NormRope(torch.autograd.Function):
         return dqkv, None, None, None
 
 
+class Embed(torch.autograd.Function):
+    """Rows of the embedding `w`; its gradient goes to `grad`."""
+
+    @staticmethod
+    def forward(ctx, w, prog, grad):
+        x = torch.empty((BATCH, TOKENS, HIDDEN), dtype=BF16, device=DEV)
+        ops.sdp_embed(prog.ctx, w, prog.tokens.flatten(), x.flatten(0, 1), stream=torch.cuda.current_stream())
+        ctx.saved = prog, grad
+        return x
+
+    @staticmethod
+    def backward(ctx, dx):
+        prog, grad = ctx.saved
+        ops.sdp_embed_backward(prog.ctx, dx.reshape(-1, HIDDEN), prog.tokens.flatten(), grad,
+                               stream=torch.cuda.current_stream())
+        return None, None, None
+
+
+class Route(torch.autograd.Function):
+    """Each token's chosen experts and their shares of it."""
+
+    @staticmethod
+    def forward(ctx, logits, prog):
+        share = torch.empty((logits.shape[0], TOP), device=DEV)
+        chosen = torch.empty((logits.shape[0], TOP), dtype=torch.int32, device=DEV)
+        ops.sdp_route(prog.ctx, logits, chosen, share, stream=torch.cuda.current_stream())
+        ctx.saved = prog, logits, chosen
+        ctx.mark_non_differentiable(chosen)
+        return share, chosen
+
+    @staticmethod
+    def backward(ctx, dshare, _):
+        prog, logits, chosen = ctx.saved
+        dlogits = torch.empty_like(logits)
+        ops.sdp_route_backward(prog.ctx, logits, chosen, dshare.contiguous(), dlogits,
+                               stream=torch.cuda.current_stream())
+        return dlogits, None
+
+
+class Gather(torch.autograd.Function):
+    """Tokens to their entries' rows, which are sorted by expert."""
+
+    @staticmethod
+    def forward(ctx, x, place, prog):
+        rows = torch.empty((place.numel(), HIDDEN), dtype=BF16, device=DEV)
+        ops.sdp_expert_gather(prog.ctx, x, place, rows, stream=torch.cuda.current_stream())
+        ctx.saved = prog, place
+        return rows
+
+    @staticmethod
+    def backward(ctx, drows):
+        prog, place = ctx.saved
+        dx = torch.empty((place.shape[0], HIDDEN), dtype=BF16, device=DEV)
+        ops.sdp_expert_gather_backward(prog.ctx, drows.contiguous(), place, dx, stream=torch.cuda.current_stream())
+        return dx, None, None
+
+
+class Combine(torch.autograd.Function):
+    """The stream and the experts' rows, each by its share."""
+
+    @staticmethod
+    def forward(ctx, x, rows, share, place, prog):
+        out = torch.empty_like(x)
+        ops.sdp_expert_combine(prog.ctx, rows, place, share, out, residual=x, stream=torch.cuda.current_stream())
+        ctx.saved = prog, rows, share, place
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        prog, rows, share, place = ctx.saved
+        drows, dshare = torch.empty_like(rows), torch.empty_like(share)
+        ops.sdp_expert_combine_backward(prog.ctx, rows, place, share, dout.contiguous(), drows, dshare,
+                                        stream=torch.cuda.current_stream())
+        return dout, drows, dshare, None, None
+
+
 class Experts(torch.autograd.Function):
     """Rows sorted by expert times that expert's weight; its gradient goes to `grad`."""
 
@@ -115,7 +193,7 @@ class Program:
         """Logits of every token; `leaf`: the weights that plain torch differentiates."""
         g = grads if grads is not None else {n: torch.empty_like(t) for n, t in weights.w.items()}
         w = weights.w
-        x = leaf["embed"][self.tokens]
+        x = Embed.apply(leaf["embed"], self, g["embed"])
         qkv = (x.flatten(0, 1) @ leaf["qkv"].t()).view(BATCH, TOKENS, Q_HEADS + 2 * K_HEADS, DIM)
         q, k = NormRope.apply(qkv, self, w, g)
         v = qkv[:, :, Q_HEADS + K_HEADS:]
@@ -126,21 +204,21 @@ class Program:
         a = score.masked_fill(later, float("-inf")).softmax(-1) @ v
         x = x + (a.transpose(1, 2).reshape(BATCH * TOKENS, -1).to(BF16) @ leaf["o"].t()).view_as(x)
         x = x.flatten(0, 1)
-        share, chosen = (x @ leaf["router"].t()).float().softmax(-1).topk(TOP, dim=-1)
-        order = chosen.flatten().argsort(stable=True)
-        ends = torch.bincount(chosen.flatten(), minlength=EXPERTS).cumsum(0)
-        rows = x[order // TOP]
+        share, chosen = Route.apply(x @ leaf["router"].t(), self)
+        place = torch.empty_like(chosen)
+        ends = torch.empty(EXPERTS, dtype=torch.int64, device=DEV)
+        ops.sdp_expert_order(self.ctx, chosen, ends, place, stream=torch.cuda.current_stream())
+        rows = Gather.apply(x, place, self)
         gate, up = Experts.apply(rows, self, w["up"], g["up"], ends).chunk(2, dim=1)
         h = (torch.nn.functional.silu(gate.float()) * up.float()).to(BF16)
         y = Experts.apply(h, self, w["down"], g["down"], ends)
-        y = y.float() * share.flatten()[order][:, None]
-        x = x + torch.zeros_like(x, dtype=torch.float32).index_add(0, order // TOP, y).to(BF16)
+        x = Combine.apply(x, y, share, place, self)
         return x @ leaf["head"].t()
 
     def step(self, number, lr):
         s = self.student
-        mine = ("q_norm", "k_norm", "up", "down")  # whose gradients the operators write
-        leaf = {n: t if n in mine else t.detach().requires_grad_() for n, t in s.w.items()}
+        mine = ("embed", "q_norm", "k_norm", "up", "down")  # whose gradients the operators write
+        leaf = {n: t.detach().requires_grad_() for n, t in s.w.items()}
         logits = self.forward(s, leaf, s.g)
         loss = torch.empty(logits.shape[0], device=DEV)
         row_grad = torch.full_like(loss, 1.0 / int(self.learned.sum()))
