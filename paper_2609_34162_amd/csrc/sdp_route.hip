@@ -228,9 +228,10 @@ __device__ __forceinline__ float without_place(float key) { return __uint_as_flo
 // each other are close (and not from the same logit and bias) more experts are taken until
 // the next one is far enough, and these candidates are ranked by their scores in 64 bits;
 // close groups are compared in 64 bits likewise.  A token that has too many candidates, a
-// NaN or an infinite key is done the slow way, behind the others.  Of 32,768 tokens' 256
-// sigmoid scores with a bias, one in about 100 needs the ranking, one in some thousands
-// its groups compared.
+// NaN or an infinite key is done the slow way, behind the others: one such token makes a
+// call 17 us longer.  Of 32,768 tokens' 256 sigmoid scores with a bias, one in about 100
+// needs the ranking, one in some thousands its groups compared (19.3 us, of which the
+// logits' bytes take 7; without the 64 bits 17.1).
 // KEEP: how many of its keys a lane's list keeps.  WIDE: a token has 32 or 64 lanes, else
 // 8 or 16.
 template <typename T, int N, int KEEP, bool WIDE, bool SCORED>
@@ -268,9 +269,6 @@ __global__ __launch_bounds__(256) void k_route_lanes(RouteArgs a) {
     auto off = [=](float key) { return SCORED ? (1.0f + fabsf(key)) * slack : 0x1p-19f * fabsf(key); };
     auto there = [](float key) { return key >= -__FLT_MAX__; };
 
-    // in a large call some of the first waves go the rare ways for nothing, so that their
-    // instructions are there when they are needed (32,768 tokens: 34.5 us, else 38.8)
-    const bool warm = gridDim.x > 1024 && blockIdx.x < 512 && wave == 0;
     const int64_t w = a.first + (int64_t)blockIdx.x * (blockDim.x >> 6) + wave;
     if (w << tokens_log >= a.tokens) return;
     const int64_t t = (w << tokens_log) + (lane / G);
@@ -369,7 +367,7 @@ __global__ __launch_bounds__(256) void k_route_lanes(RouteArgs a) {
         }
         const float next = most_of(left);
         const bool close = on && next != kNegInf && last - next <= 2.0f * off(last);
-        if (warm || __any(close && !slow)) {
+        if (__any(close && !slow)) {
             // the groups' worth in 64 bits, of the same experts (unless the next one is close to them)
             float best[3] = {kNegInf, kNegInf, kNegInf};
             int from[2] = {0, 0};
@@ -436,20 +434,21 @@ __global__ __launch_bounds__(256) void k_route_lanes(RouteArgs a) {
         // of negative keys are sorted the highest first)
         const bool same = x == next_x && b == next_b && sub + 1 < a.top && my_key > 0.0f;
         const bool close = on && has && sub < a.top && there(next) && !same && my_key - next <= off(my_key);
-        if (warm || __any(close && !slow)) {
+        if (__any(close && !slow)) {
             // candidates until the next one is far behind the last one chosen
             const float last = __shfl(my_key, token_lane + a.top - 1);
+            const float behind = __shfl(my_key, token_lane + rounds - 1);
             int count = rounds;
-            bool more = (half_of(__ballot(close)) & mask) != 0;
-            const int most_count = KEEP == N ? G : min(G, KEEP);
+            bool more = (half_of(__ballot(close)) & mask) != 0 && there(behind) && behind >= last - off(last);
 #pragma unroll 1
-            for (; count < most_count; ++count) {
+            for (; count < G && __any(more && !slow); ++count) {
+                // (a lane whose list has run out may have had more)
+                if (KEEP < N)
+                    slow = slow || (more && (half_of(__ballot(list[0] == kNegInf && list[1] == kNegInf)) & mask));
                 const float after = take(count);
                 more = more && there(after) && after >= last - off(last);
-                if (!__any(more && !slow)) break;
             }
             slow = slow || more;
-            count = min(count + 1, most_count);
             wave_fence();
             has = there(my_key) && sub < count;
             mine = has ? chosen[sub] : -1;
@@ -646,8 +645,8 @@ __global__ __launch_bounds__(64) void k_route_back_any(RouteArgs a) {
 }
 
 // Lanes of a token and experts of a lane, 16 where the lanes' lists keep nine of them.
-// The fewest lanes that the experts, the choice and the groups allow: 8,192 waves' worth of
-// 32,768 tokens' 256 experts took 44.6 us with 16 lanes of 16 and 59.4 with 32 of 8.
+// The fewest lanes that the experts, the choice and the groups allow: 32,768 tokens of 256
+// experts in groups take 19.3 us with 16 lanes of 16 and 26.7 with 32 of 8.
 // 0 lanes: none.
 struct Split {
     int lanes, each;

@@ -105,6 +105,25 @@ def test_close_scores(ctx, sigmoid):
     check(ctx, z, 8, bias, sigmoid, 8, 3, 2, renormalize=True)
 
 
+@pytest.mark.parametrize("above", [0, 5, 7, 8])
+@pytest.mark.parametrize("size", [2, 9, 10, 15, 17, 40])
+def test_clusters_of_close_scores(ctx, size, above):
+    """The choice ends before, in or behind a cluster, whose experts follow each other or lie apart."""
+    gen = torch.Generator().manual_seed(size)
+    e, t = 256, 60
+    z = -3.0 + torch.rand((t, e), generator=gen)
+    for i in range(t):
+        start = int(torch.randint(0, e - size, (1,), generator=gen))
+        at = torch.arange(start, start + size) if i % 2 else torch.randperm(e, generator=gen)[:size]
+        z[i, at] = 1.0 + 2.0 ** -23 * torch.randperm(size, generator=gen)
+        z[i, (at[-1] + 1 + 7 * torch.arange(above)) % e] = 2.0 + 0.1 * torch.arange(above)
+    z, bias = z.cuda(), (1e-7 * torch.randn(e, generator=gen)).cuda()
+    for sigmoid in (False, True):
+        check(ctx, z, 8, None, sigmoid)
+        check(ctx, z, 8, bias, sigmoid, renormalize=True)
+        check(ctx, z, 8, bias, sigmoid, 8, 4, 2)
+
+
 @pytest.mark.parametrize("sigmoid,renormalize", list(itertools.product([False, True], [False, True])))
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_masked_experts(ctx, sigmoid, renormalize, dtype):
