@@ -25,6 +25,7 @@
  * sums in FP32 and each output rounded once; the same inputs give the same
  * bits (the only atomics count integers in LDS); sizes of zero are valid;
  * values in device memory that are out of range are never used as an address.
+ * hidden is at most 2^30; scale, eps and weight_offset are finite in FP32.
  *
  * sdp_embed_backward and sdp_block_norm_backward with gradients that are sums
  * over tokens (weights, a gate that tokens share) use the context's workspace:

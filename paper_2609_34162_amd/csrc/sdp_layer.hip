@@ -16,6 +16,12 @@ int need(const char *call, const sdp_ctx *ctx, const void *desc) {
     return SDP_OK;
 }
 
+// Kernels count in 32 bits within a row.
+constexpr int32_t kMostHidden = 1 << 30;
+
+// Finite as what the kernels take.
+bool is_finite(double v) { return std::isfinite((float)v); }
+
 Rows kernel_rows(const sdp_rows *r) { return r ? Rows{r->data, r->stride} : Rows{nullptr, 0}; }
 
 // Adds a [rows, cols] tensor to a call's; absent ones have no elements.
@@ -31,11 +37,11 @@ int embed_call(sdp_ctx *ctx, const char *call, const sdp_embed_desc *d, const sd
                bool backward, int32_t accumulate, void *stream) {
     SDP_TRY(need(call, ctx, d));
     if (!table || !rows) return fail(SDP_ERR_INVALID_ARGUMENT, "%s: a tensor is NULL", call);
-    if (d->tokens < 0 || d->tokens > INT32_MAX || d->vocab < 0 || d->hidden < 0)
+    if (d->tokens < 0 || d->tokens > INT32_MAX || d->vocab < 0 || d->hidden < 0 || d->hidden > kMostHidden)
         return fail(SDP_ERR_INVALID_ARGUMENT, "%s: tokens, vocab or hidden out of range", call);
     if (!is_float_type(d->table_type) || !is_float_type(d->row_type) || !is_int_type(d->id_type))
         return fail(SDP_ERR_INVALID_ARGUMENT, "%s: a type is none of those allowed", call);
-    if (!std::isfinite(d->scale)) return fail(SDP_ERR_INVALID_ARGUMENT, "%s: scale must be finite", call);
+    if (!is_finite(d->scale)) return fail(SDP_ERR_INVALID_ARGUMENT, "%s: scale must be finite", call);
     std::vector<Tensor> ts;
     add(ts, backward ? "dtable" : "table", table, d->vocab, d->hidden, d->table_type, backward);
     add(ts, backward ? "dout" : "out", rows, d->tokens, d->hidden, d->row_type, !backward);
@@ -71,15 +77,15 @@ int embed_call(sdp_ctx *ctx, const char *call, const sdp_embed_desc *d, const sd
 
 int check_norm(const char *call, sdp_ctx *ctx, const sdp_block_norm_desc *d) {
     SDP_TRY(need(call, ctx, d));
-    if (d->tokens < 0 || d->tokens > INT32_MAX || d->hidden < 0)
+    if (d->tokens < 0 || d->tokens > INT32_MAX || d->hidden < 0 || d->hidden > kMostHidden)
         return fail(SDP_ERR_INVALID_ARGUMENT, "%s: tokens or hidden out of range", call);
     if (!is_float_type(d->stream_type) || !is_float_type(d->type) || !is_float_type(d->weight_type))
         return fail(SDP_ERR_INVALID_ARGUMENT, "%s: a type is none of those allowed", call);
     if (d->gate_form < SDP_GATE_NONE || d->gate_form > SDP_GATE_ELEMENT)
         return fail(SDP_ERR_INVALID_ARGUMENT, "%s: gate_form is none of those allowed", call);
-    if (!std::isfinite(d->eps) || d->eps < 0.0)
+    if (!is_finite(d->eps) || d->eps < 0.0)
         return fail(SDP_ERR_INVALID_ARGUMENT, "%s: eps must be finite and >= 0", call);
-    if (!std::isfinite(d->scale) || !std::isfinite(d->weight_offset))
+    if (!is_finite(d->scale) || !is_finite(d->weight_offset))
         return fail(SDP_ERR_INVALID_ARGUMENT, "%s: scale and weight_offset must be finite", call);
     return SDP_OK;
 }
@@ -126,7 +132,7 @@ int check_route(const char *call, sdp_ctx *ctx, const sdp_route_desc *d, bool gr
                     SDP_ROUTE_MAX_TOP, d->top);
     if (!is_float_type(d->logit_type) || !is_int_type(d->index_type) || !is_float_type(d->weight_type))
         return fail(SDP_ERR_INVALID_ARGUMENT, "%s: a type is none of those allowed", call);
-    if (!std::isfinite(d->scale)) return fail(SDP_ERR_INVALID_ARGUMENT, "%s: scale must be finite", call);
+    if (!is_finite(d->scale)) return fail(SDP_ERR_INVALID_ARGUMENT, "%s: scale must be finite", call);
     if (!groups) return SDP_OK;
     if (d->groups < 1 || d->groups > SDP_ROUTE_MAX_GROUPS || d->experts % d->groups != 0)
         return fail(SDP_ERR_INVALID_ARGUMENT, "%s: groups must divide experts and be in 1..%d (got %d)", call,
@@ -158,7 +164,7 @@ RouteArgs route_args(const sdp_route_desc *d, const void *logits) {
 
 int check_experts(const char *call, sdp_ctx *ctx, const sdp_expert_desc *d, int64_t *entries) {
     SDP_TRY(need(call, ctx, d));
-    if (d->tokens < 0 || d->top < 0 || d->hidden < 0 || d->tokens > INT32_MAX ||
+    if (d->tokens < 0 || d->top < 0 || d->hidden < 0 || d->hidden > kMostHidden || d->tokens > INT32_MAX ||
         (*entries = d->tokens * d->top) > INT32_MAX)
         return fail(SDP_ERR_INVALID_ARGUMENT, "%s: tokens, top or hidden out of range", call);
     if (!is_float_type(d->row_type) || !is_float_type(d->stream_type) || !is_float_type(d->weight_type))

@@ -44,6 +44,7 @@ def test_embed(lib):
     refused(ops, bad, "out overlaps itself", f, ctx, table, ids, out[:1].expand(6, 16))
     refused(ops, bad, "out overlaps table", f, ctx, table, ids, table[2:8])
     refused(ops, bad, "scale must be finite", f, ctx, table, ids, out, scale=float("inf"))
+    refused(ops, bad, "scale must be finite", f, ctx, table, ids, out, scale=1e39)
     refused(ops, bad, "dtable overlaps dout", b, ctx, table[:6], ids, table)
     refused(ops, bad, "dtable overlaps itself", b, ctx, out, ids, table[:1].expand(10, 16))
     d = ops.sdp_embed_desc(1 << 28, 10, 16, ops.SDP_TYPE_F32, ops.SDP_TYPE_F32, ops.SDP_TYPE_I64, ids.data_ptr(), 1.0)
@@ -54,7 +55,9 @@ def test_embed(lib):
     refused(ops, bad, "out of range", call)
     d.tokens, o.stride = 6, -16
     refused(ops, bad, "stride", call)
-    o.stride, o.data = 16, out.data_ptr() + 2
+    o.stride, d.hidden = 16, (1 << 30) + 1
+    refused(ops, bad, "hidden out of range", call)
+    d.hidden, o.data = 16, out.data_ptr() + 2
     refused(ops, align, "aligned", call)
     d.row_type = 3
     refused(ops, bad, "type", call)
@@ -76,6 +79,7 @@ def test_block_norm(lib):
     refused(ops, bad, "h_out without y", f, ctx, h, None, ho, no)
     refused(ops, bad, "eps", f, ctx, h, y, ho, no, eps=-1.0)
     refused(ops, bad, "finite", f, ctx, h, y, ho, no, scale=float("nan"))
+    refused(ops, bad, "finite", f, ctx, h, y, ho, no, weight_offset=-1e39)
     refused(ops, bad, "h_out overlaps n_out", f, ctx, h, y, ho, ho)
     refused(ops, bad, "n_out overlaps h", f, ctx, h, y, ho, h)
     refused(ops, bad, "h_out overlaps y", f, ctx, h, y, y, no)
@@ -100,7 +104,11 @@ def test_block_norm(lib):
     grads = ops.sdp_block_norm_grads(r(dh), r(dy), dw.data_ptr(), 0, None, None)
     refused(ops, bad, "dgate without a gate", lambda: sdp._check(sdp._lib.sdp_block_norm_backward(
         ctx, ctypes.byref(d), r(h), r(y), r(ho), r(no), ctypes.byref(grads), None)))
-    d.gate_form = 9
+    for tokens, hidden in ((1 << 31, 16), (6, (1 << 30) + 1)):
+        d.tokens, d.hidden = tokens, hidden
+        refused(ops, bad, "out of range", lambda: sdp._check(sdp._lib.sdp_block_norm(
+            ctx, ctypes.byref(d), r(h), r(y), r(ho), r(no), None)))
+    d.tokens, d.hidden, d.gate_form = 6, 16, 9
     refused(ops, bad, "gate_form", lambda: sdp._check(sdp._lib.sdp_block_norm(
         ctx, ctypes.byref(d), r(h), r(y), r(ho), r(no), None)))
     assert all((t == 7).all() for t in (ho, no, dh, dy, dw))
@@ -158,7 +166,9 @@ def test_experts(lib):
     d = ops.sdp_expert_desc(1 << 20, 1 << 12, 16, 0, 0, 0, own.data_ptr())
     r = lambda t: ctypes.pointer(ops.sdp_rows(t.data_ptr(), 16))
     refused(ops, bad, "out of range", lambda: sdp._check(sdp._lib.sdp_expert_gather(ctx, ctypes.byref(d), r(x), r(rows), None)))
-    d.tokens, d.top = 6, 2
+    d.tokens, d.top, d.hidden = 6, 2, (1 << 30) + 1
+    refused(ops, bad, "out of range", lambda: sdp._check(sdp._lib.sdp_expert_gather(ctx, ctypes.byref(d), r(x), r(rows), None)))
+    d.hidden = 16
     refused(ops, bad, "weights is NULL", lambda: sdp._check(sdp._lib.sdp_expert_combine(
         ctx, ctypes.byref(d), r(rows), None, None, r(out), None)))
     assert (ends == 7).all() and (place == 7).all() and (rows == 7).all() and (out == 7).all()
