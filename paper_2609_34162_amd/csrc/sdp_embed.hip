@@ -152,7 +152,8 @@ __device__ __forceinline__ int64_t lower_bound(const EmbedArgs &a, int64_t v) {
 
 // What the pieces have not written: rows of no token, and of runs over several pieces.
 // A block takes ROWS rows, whose 16-byte parts its threads walk one after the other
-// (151,936 x 4,096 in BF16, of which 32,768 tokens reach a sixth: 228 us, of one wave a row 330).
+// (a wave to a row: 318 us for the call's 309 below).  Zeros are stored plainly, which is
+// quicker than with the non-temporal hint (321).
 constexpr int kTableThreads = 256;
 template <typename T, int ROWS, bool ONCE>
 __global__ __launch_bounds__(kTableThreads) void k_embed_table(EmbedArgs a) {
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(kTableThreads) void k_embed_table(EmbedArgs a) {
             T *out = (T *)a.table.data + (v0 + row) * a.table.stride + c;
             if (p0 == p1) {
                 if (left == kPer)
-                    store_any16<ONCE>(out, u32x4{0, 0, 0, 0});
+                    store_any16<false>(out, u32x4{0, 0, 0, 0});
                 else
                     for (int k = 0; k < left; ++k) out[k] = 0;
                 continue;
@@ -287,7 +288,6 @@ hipError_t launch_embed_backward(const EmbedArgs &args, bool table_bf16, bool ro
         };
         once ? pick(std::true_type()) : pick(std::false_type());
     }
-    // rows of a block: about 64 KB, so that finding them costs little beside them
     auto table = [&](auto rows) {
         constexpr int ROWS = decltype(rows)::value;
         const dim3 grid((uint32_t)std::min<int64_t>(((int64_t)a.vocab + ROWS - 1) / ROWS, 1 << 20));
@@ -297,10 +297,13 @@ hipError_t launch_embed_backward(const EmbedArgs &args, bool table_bf16, bool ro
         else
             once ? go(k_embed_table<float, ROWS, true>) : go(k_embed_table<float, ROWS, false>);
     };
-    if ((int64_t)a.hidden * (table_bf16 ? 2 : 4) > 1024)
-        table(std::integral_constant<int, 32>());
+    // rows of a block: few, so that blocks at work write close together, but enough of short
+    // rows that finding them costs little (151,936 rows of 8 KB: 309 us in fours, 348 in 32s;
+    // of 1.3 KB 123 and 94)
+    if ((int64_t)a.hidden * (table_bf16 ? 2 : 4) > 1536)
+        table(std::integral_constant<int, 4>());
     else
-        table(std::integral_constant<int, 128>());
+        table(std::integral_constant<int, 64>());
     return hipGetLastError();
 }
 
