@@ -1,5 +1,6 @@
 """Register and scratch use of the kernels around the experts' products, from the
-compiler's resource report (no GPU needed): none may use scratch memory."""
+compiler's resource report (no GPU needed): none may use scratch memory, and those
+that memory bounds keep the waves that hide its latency."""
 import os
 import re
 import shutil
@@ -44,3 +45,11 @@ def report(tmp_path_factory):
 def test_no_scratch(report):
     bad = {k: v["ScratchSize"] for k, v in report.items() if v["ScratchSize"]}
     assert not bad, bad
+
+
+@pytest.mark.parametrize("kernel,waves", [("k_norm_rowsIttLi1ELb1E", 7), ("k_norm_back_rowsIttLb0E", 4), ("k_route_lanesI", 5),
+                                          ("k_gatherI", 8), ("k_combineILi64EttL", 8), ("k_combine_backI", 7),
+                                          ("k_embed_tableItLi4E", 4), ("k_embed_piecesIttL", 4)])
+def test_occupancy(report, kernel, waves):
+    found = {k: v["Occupancy"] for k, v in report.items() if kernel in k}
+    assert found and min(found.values()) >= waves, found
