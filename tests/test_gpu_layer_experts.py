@@ -59,6 +59,13 @@ def test_order_of_experts(ctx, experts):
         check_order(ctx, choice(n, 1, experts, seed=experts), experts)
 
 
+@pytest.mark.parametrize("n", [1024, 1025, 40960, 40961, 131072, 131073])
+@pytest.mark.parametrize("experts", [128, 511, 512, 1024, 2048])
+def test_order_around_its_ways(ctx, n, experts):
+    """One block, one launch and three launches; few digits and many."""
+    check_order(ctx, choice(n, 1, experts, seed=n + experts), experts)
+
+
 def test_order_of_skewed_choices(ctx):
     for index in (torch.zeros(9000, 1), torch.full((9000, 1), 15), torch.full((9000, 1), -1),
                   torch.arange(9000)[:, None] % 16, 15 - torch.arange(9000)[:, None] * 16 // 9000):
@@ -276,3 +283,33 @@ def test_same_bits_again_and_on_another_stream(ctx):
         got.append((ends, place, out, dy, dw))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for other in got[1:] for a, b in zip(got[0], other))
+
+
+def test_gradients_against_differences(ctx):
+    """<gradient, direction> against differences of <output, its gradient> in 64 bits; each output
+    is linear in each input, so they are exact."""
+    from paper_2609_34162_amd import ops
+    gen = torch.Generator().manual_seed(6)
+    t, k, experts, h = 40, 3, 7, 70
+    _, place, _ = sort(ctx, choice(t, k, experts, 0.2, 2).to(I32).cuda(), experts)
+    make = lambda *shape: torch.randn(shape, generator=gen).cuda()
+    y, w, dout, drows = make(t * k, h), make(t, k), make(t, h), make(t * k, h)
+    dy, dw, dx = torch.empty_like(y), torch.empty_like(w), torch.empty_like(dout)
+    ops.sdp_expert_combine_backward(ctx, y, place, w, dout, dy, dw)
+    ops.sdp_expert_gather_backward(ctx, drows, place, dx)
+
+    def combined(rows64, weights64):
+        return (ref.combine(rows64, place, weights64, None, F32)[0] * ref.f64(dout)).sum()
+
+    def gathered(x64):
+        return (ref.f64(ref.gather(x64, place)) * ref.f64(drows)).sum()
+    vy, vw, vx = (torch.randn(s.shape, generator=gen).double() for s in (y, w, dout))
+    y64, w64, x64 = ref.f64(y), ref.f64(w), torch.zeros((t, h), dtype=torch.float64)
+    # each gradient: a rounded product, a sum of 70 of them, or of three rows
+    dw_size = ref.combine_back(y.abs(), place, w, dout.abs(), F32, F32)[1][0]
+    dx_size = ref.combine(drows.abs(), place, None, None, F32)[0]
+    for got, v, want, size, count in (
+            (dy, vy, combined(y64 + vy, w64) - combined(y64, w64), dy, 2),
+            (dw, vw, combined(y64, w64 + vw) - combined(y64, w64), dw_size, h + 2),
+            (dx, vx, gathered(x64 + vx) - gathered(x64), dx_size, k + 1)):
+        assert abs((ref.f64(got) * v).sum() - want) <= (count * ref.U32 + 1e-12) * (ref.f64(size).abs() * v.abs()).sum()
