@@ -14,6 +14,7 @@
 
 #include "sdp_layer_device.h"
 #include "sdp_layer_internal.h"
+#include "sdp_route_keys.h"
 
 namespace sdpops {
 namespace {
@@ -212,14 +213,6 @@ __device__ __forceinline__ void sort_list(float *v) {
                     }
 }
 
-// A key is a float whose last four bits say where in its lane the expert is, so that a
-// lane's keys are sorted by maxima and minima alone.
-constexpr uint32_t kPlace = 15;
-__device__ __forceinline__ float with_place(float key, uint32_t place) {
-    return __uint_as_float((__float_as_uint(key) & ~kPlace) | place);
-}
-__device__ __forceinline__ float without_place(float key) { return __uint_as_float(__float_as_uint(key) & ~kPlace); }
-
 // `lanes` lanes take a token, a lane N experts that follow each other.  Each lane sorts
 // its keys; then the largest first key of the lanes is taken `top` times, and its lane
 // moves its list on.
@@ -321,9 +314,7 @@ __global__ __launch_bounds__(256) void k_route_lanes(RouteArgs a) {
         for (int i = 0; i < N; ++i) {
             const float key = z[i] == kNegInf || !SCORED ? z[i] : list[i];
             finite = finite && key < __builtin_huge_valf();
-            uint32_t place = kPlace - i;
-            if (kExact) place = __float_as_uint(key) >> 31 ? i : place;  // equals: the lowest first
-            list[i] = key == kNegInf ? key : with_place(kExact ? key + 0.0f : key, place);
+            list[i] = key_of<kExact>(key, i);
         }
     }
     sort_list<N>(list);
@@ -375,7 +366,7 @@ __global__ __launch_bounds__(256) void k_route_lanes(RouteArgs a) {
 #pragma unroll
                 for (int k = 0; k < 3; ++k) {
                     const float v = of[l][k];
-                    const int e = (sub * group_lanes + l) * N + (int)(~__float_as_uint(v) & kPlace);
+                    const int e = (sub * group_lanes + l) * N + (int)place_of<false>(v);
                     if (v > best[0]) {
                         best[2] = best[1], best[1] = best[0], from[1] = from[0];
                         best[0] = v, from[0] = e;
@@ -413,8 +404,7 @@ __global__ __launch_bounds__(256) void k_route_lanes(RouteArgs a) {
         const bool mine = first == most && most != kNegInf;
         const bool owner = mine && !(half_of(__ballot(mine)) & below);
         my_key = sub == j ? most : my_key;
-        const uint32_t bits = __float_as_uint(list[0]), place = kExact && bits >> 31 ? bits : ~bits;
-        chosen[owner ? j : nowhere] = e0 + (int)(place & kPlace);
+        chosen[owner ? j : nowhere] = e0 + (int)place_of<kExact>(list[0]);
 #pragma unroll
         for (int i = 0; i + 1 < KEEP; ++i) list[i] = owner ? list[i + 1] : list[i];
         list[KEEP - 1] = owner ? kNegInf : list[KEEP - 1];
