@@ -339,25 +339,24 @@ __global__ __launch_bounds__(256) void k_route_lanes(RouteArgs a) {
         for (int k = 0; k < 3; ++k) best_of[wave][lane][k] = k < N ? list[k < N ? k : 0] : kNegInf;
         wave_fence();
         const float(*const of)[3] = best_of[wave] + token_lane + sub * group_lanes;
-        float worth = kNegInf;
-        if (sub < a.groups) {
-            float first = kNegInf, second = kNegInf;
-            for (int l = 0; l < group_lanes; ++l) {
-                second = fmaxf(fmaxf(second, of[l][1]), fminf(first, of[l][0]));
-                first = fmaxf(first, of[l][0]);
-            }
-            worth = a.group_best > 1 && second != kNegInf ? first + second : first;
+        float first = kNegInf, second = kNegInf;
+        for (int l = 0; l < (sub < a.groups ? group_lanes : 0); ++l) {
+            second = fmaxf(fmaxf(second, of[l][1]), fminf(first, of[l][0]));
+            first = fmaxf(first, of[l][0]);
         }
+        const Worth worth = worth_of(first, a.group_best > 1 ? second : kNegInf);
         bool kept = false;
-        float last = kNegInf, left = worth;
+        float left = worth.value;
         for (int k = 0; k < a.top_groups; ++k) {
-            last = most_of(left);
-            const bool mine = left == last, owner = mine && !(half_of(__ballot(mine)) & below);
+            const float most = most_of(left);
+            const bool mine = left == most, owner = mine && !(half_of(__ballot(mine)) & below);
             kept = kept || owner;
             left = owner ? kNegInf : left;
         }
-        const float next = most_of(left);
-        const bool close = on && next != kNegInf && last - next <= 2.0f * off(last);
+        // one that is left may be worth as much as one that is kept
+        const float high = most_of(left + worth.room),
+                    low = -most_of(kept && there(worth.value) ? worth.room - worth.value : kNegInf);
+        const bool close = on && high != kNegInf && low <= high;
         if (__any(close && !slow)) {
             // the groups' worth in 64 bits, of the same experts (unless the next one is close to them)
             float best[3] = {kNegInf, kNegInf, kNegInf};

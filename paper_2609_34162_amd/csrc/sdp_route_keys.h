@@ -31,4 +31,20 @@ constexpr uint32_t place_of(float key) {
     return (EXACT && bits >> 31 ? bits : ~bits) & kPlace;
 }
 
+// A group's worth, of its two best keys (or one; minus infinity: not there), and how far
+// it may be from that of the scores and biases themselves.  A key's four bits, its sum with
+// the bias and the worth's own addition are 33 roundings in proportion to the keys, which
+// may cancel in the worth; the scores, the sum of a softmax most of them, are off by 40
+// roundings of one.  (Taken as 48 of each.)
+struct Worth {
+    float value, room;
+};
+constexpr float size_of(float v) { return v < 0.0f ? -v : v; }
+constexpr Worth worth_of(float first, float second) {
+    constexpr float kNone = -__builtin_huge_valf();
+    if (first == kNone) return {kNone, 0.0f};
+    if (second == kNone) second = 0.0f;
+    return {first + second, (1.0f + size_of(first) + size_of(second)) * 0x1.8p-19f};
+}
+
 }  // namespace sdpops
