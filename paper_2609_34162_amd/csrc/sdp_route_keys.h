@@ -31,8 +31,9 @@ constexpr uint32_t place_of(float key) {
     return (EXACT && bits >> 31 ? bits : ~bits) & kPlace;
 }
 
-// A group's worth, of its two best keys (or one; minus infinity: not there), and how far
-// it may be from that of the scores and biases themselves.  A key's four bits, its sum with
+// Half of a group's worth, of its two best keys (or one; minus infinity: not there), and
+// how far it may be from that of the scores and biases themselves.  (The sum of two lowest
+// values, or of two largest ones, is past FP32; half of it is not.)  A key's four bits, its sum with
 // the bias and the worth's own addition are 33 roundings in proportion to the keys, which
 // may cancel in the worth; the scores, the sum of a softmax most of them, are off by 40
 // roundings of one.  (Taken as 48 of each.)
@@ -44,7 +45,7 @@ constexpr Worth worth_of(float first, float second) {
     constexpr float kNone = -__builtin_huge_valf();
     if (first == kNone) return {kNone, 0.0f};
     if (second == kNone) second = 0.0f;
-    return {first + second, (1.0f + size_of(first) + size_of(second)) * 0x1.8p-19f};
+    return {0.5f * first + 0.5f * second, (0.5f + 0.5f * size_of(first) + 0.5f * size_of(second)) * 0x1.8p-19f};
 }
 
 }  // namespace sdpops

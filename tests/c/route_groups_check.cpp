@@ -47,13 +47,26 @@ int main() {
                 const double shift = a.exact - b.exact;
                 if (size < 1e6) {
                     const float by = (float)(shift * (1 + 4e-6 * (uniform() - 0.5)));
-                    b.exact += by, b.worth.value += by;
+                    b.exact += by, b.worth.value += 0.5f * by;  // (half of the worth)
                 }
                 const bool other = (a.exact < b.exact) != (a.worth.value < b.worth.value);
                 turned += other;
                 bad += other && std::fabs((double)a.worth.value - b.worth.value) >
                                     ((double)a.worth.room + b.worth.room);
             }
+    // at the ends of FP32: numbers, in the order of their sums in 64 bits
+    const float most = 0x1.fffffep127f, ends[] = {-most, -0.7f * most, -1e30f, -1.0f, 0.0f, 2.0f, 1e30f, 0.7f * most, most};
+    for (float a : ends)
+        for (float b : ends)
+            for (float c : ends)
+                for (float d : ends) {
+                    const Worth x = worth_of(a, b), y = worth_of(c, d);
+                    bad += !std::isfinite(x.value) || !std::isfinite(x.room);
+                    const double sx = (double)a + b, sy = (double)c + d;
+                    bad += sx > sy && y.value > x.value && (double)y.value - y.room > (double)x.value + x.room;
+                }
+    const Worth none = worth_of(-HUGE_VALF, -HUGE_VALF), one = worth_of(-most, -HUGE_VALF);
+    bad += none.value != -HUGE_VALF || none.room != 0.0f || one.value != -0.5f * most;
     if (turned < 1000) std::printf("only %d came in another order\n", turned);
     if (bad) std::printf("%d of %d are not seen\n", bad, turned);
     if (!bad && turned >= 1000) std::printf("ok\n");
