@@ -23,14 +23,15 @@ __device__ __forceinline__ float weight_at(const NormArgs &a, const void *w, int
 }
 
 // A gate after its activation, and its slope by the gate's input: of a sigmoid s the slope
-// is s (1 - s) = s^2 e, e = exp(-z), which loses nothing where s is close to one.
+// is s (1 - s) = s^2 e, e = exp(-z), which loses nothing where s is close to one.  Of a NaN
+// both are NaN, which fminf loses.
 struct Gate {
     float act, slope;
 };
 __device__ __forceinline__ Gate gate_of(const NormArgs &a, float z) {
     if (!a.sigmoid) return {z, 1.0f};
     const float e = fminf(expf(-z), __FLT_MAX__), s = __builtin_amdgcn_rcpf(1.0f + e);
-    return {z != z ? z : s, s * (s * e)};
+    return {z != z ? z : s, z != z ? z : s * (s * e)};
 }
 
 // Eight of a norm's weights with their offset; zeros behind the row.
