@@ -504,6 +504,9 @@ __global__ __launch_bounds__(kSumThreads) void k_norm_sums(NormArgs a) {
     }
     if (y > 0) return;
     s = part[0][x];
+    // (without tokens the sums are zeros, whatever the gate and the weight hold: neither is read,
+    // and the call has not looked where the weight lies)
+    const bool some = a.tokens > 0;
     for (int k = 0; k < 4 && i + k < a.hidden; ++k) {
         auto put = [&](void *w, float v) {
             if (a.weight_bf16)
@@ -516,11 +519,11 @@ __global__ __launch_bounds__(kSumThreads) void k_norm_sums(NormArgs a) {
             continue;
         }
         const bool channel = a.gate_form == SDP_GATE_CHANNEL;
-        const Gate gate = channel ? gate_of(a, load1((const T *)a.gate + i + k)) : Gate{1.0f, 1.0f};
+        const Gate gate = channel && some ? gate_of(a, load1((const T *)a.gate + i + k)) : Gate{1.0f, 1.0f};
         if (a.dpost) put(a.dpost, a.scale * gate.act * s[k]);
         if (a.dgate && channel)
             store1((T *)a.dgate + i + k,
-                   a.scale * gate.slope * (a.post_norm ? weight_at(a, a.post_weight, i + k) : 1.0f) * s[k]);
+                   a.scale * gate.slope * (a.post_norm && some ? weight_at(a, a.post_weight, i + k) : 1.0f) * s[k]);
     }
 }
 
