@@ -95,7 +95,7 @@ Tensor gate_tensor(const char *what, const sdp_block_norm_desc *d, const void *p
     const int64_t size = type_size(d->type);
     switch (d->gate_form) {
         case SDP_GATE_CHANNEL: return dense(what, p, d->hidden, size, written);
-        case SDP_GATE_TOKEN: return rows_of(what, p, d->hidden ? d->tokens : 0, stride, 1, size, written);
+        case SDP_GATE_TOKEN: return rows_of(what, p, d->hidden || written ? d->tokens : 0, stride, 1, size, written);
         default: return rows_of(what, p, d->tokens, stride, d->hidden, size, written);
     }
 }
@@ -263,7 +263,6 @@ int sdp_block_norm_backward(sdp_ctx *ctx, const sdp_block_norm_desc *desc, const
         if (g.dpre_weight) ts.push_back(dense("dpre_weight", g.dpre_weight, n, wsize, true));
         DeviceGuard guard(ctx->device);
         SDP_TRY(check_tensors(ctx, call, ts, {{ho, di}, {yo, ni}, {yo, yi}}));
-        if (n == 0) return SDP_OK;
         NormArgs a = norm_args(desc, dn ? h_out : nullptr, uses_y ? y : nullptr);
         if (!gated) a.gate_form = SDP_GATE_NONE;
         if (!post) a.post_weight = nullptr;
@@ -280,6 +279,10 @@ int sdp_block_norm_backward(sdp_ctx *ctx, const sdp_block_norm_desc *desc, const
                                 g.dpost_weight || (g.dgate && desc->gate_form == SDP_GATE_CHANNEL)};
         hipStream_t s = (hipStream_t)stream;
         const bool stream_bf16 = desc->stream_type == SDP_TYPE_BF16, bf16 = desc->type == SDP_TYPE_BF16;
+        if (n == 0) {
+            HIP_TRY(launch_norm_no_channels(a, bf16, s));
+            return SDP_OK;
+        }
         a.blocks = norm_blocks(a, stream_bf16, bf16);
         const int sums = wanted[0] + wanted[1];
         if (sums) {

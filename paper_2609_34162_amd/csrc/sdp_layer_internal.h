@@ -96,6 +96,8 @@ struct NormArgs {
 int norm_blocks(const NormArgs &a, bool stream_bf16, bool bf16);
 hipError_t launch_norm(const NormArgs &a, bool stream_bf16, bool bf16, hipStream_t s);
 hipError_t launch_norm_backward(const NormArgs &a, bool stream_bf16, bool bf16, hipStream_t s);
+// What the backward call writes where hidden is 0.
+hipError_t launch_norm_no_channels(const NormArgs &a, bool bf16, hipStream_t s);
 
 // ---- routing -------------------------------------------------------------------------
 

@@ -527,6 +527,13 @@ __global__ __launch_bounds__(kSumThreads) void k_norm_sums(NormArgs a) {
     }
 }
 
+// Rows without channels: a token's gate has a gradient, the sum over nothing.
+template <typename T>
+__global__ __launch_bounds__(kAnyThreads) void k_norm_no_channels(NormArgs a) {
+    for (int64_t t = (int64_t)blockIdx.x * kAnyThreads + threadIdx.x; t < a.tokens; t += (int64_t)gridDim.x * kAnyThreads)
+        store1((T *)a.dgate + t * a.dgate_stride, 0.0f);
+}
+
 template <typename F>
 void with_types(bool stream_bf16, bool bf16, F &&go) {
     if (stream_bf16)
@@ -592,6 +599,16 @@ hipError_t launch_norm(const NormArgs &args, bool stream_bf16, bool bf16, hipStr
             return once ? go(k_norm_rows<S, T, 1, true, true, 1024>) : go(k_norm_rows<S, T, 1, true, false, 1024>);
         once ? go(k_norm_rows<S, T, 2, true, true, 1024>) : go(k_norm_rows<S, T, 2, true, false, 1024>);
     });
+    return hipGetLastError();
+}
+
+hipError_t launch_norm_no_channels(const NormArgs &a, bool bf16, hipStream_t s) {
+    if (a.tokens == 0 || !a.dgate || a.gate_form != SDP_GATE_TOKEN) return hipSuccess;
+    const dim3 grid((uint32_t)std::min<int64_t>((a.tokens + kAnyThreads - 1) / kAnyThreads, 1 << 12));
+    if (bf16)
+        hipLaunchKernelGGL((k_norm_no_channels<uint16_t>), grid, dim3(kAnyThreads), 0, s, a);
+    else
+        hipLaunchKernelGGL((k_norm_no_channels<float>), grid, dim3(kAnyThreads), 0, s, a);
     return hipGetLastError();
 }
 

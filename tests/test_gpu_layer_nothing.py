@@ -22,3 +22,15 @@ def test_no_tokens_leave_zeros_whatever_the_weights_hold(ctx, h, dtype, sigmoid)
                                 dpre_weight=dpre)
     for t in (dgate, dpost, dpre):
         assert (t == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("stride", [1, 3])
+@pytest.mark.parametrize("t", [0, 1, 7, 1000])
+def test_no_channels_leave_a_tokens_gate_zeros(ctx, t, stride, dtype):  # noqa: F811
+    from paper_2609_34162_amd import ops
+    none = torch.empty((t, 0), dtype=dtype, device="cuda")
+    gate, room = torch.randn((t, 1), device="cuda").to(dtype), torch.full((t, stride), 7.0, dtype=dtype, device="cuda")
+    ops.sdp_block_norm_backward(ctx, none, none, none, none, none.clone(), none.clone(), gate=gate, dgate=room[:, :1],
+                                gate_sigmoid=True, post_norm=True)
+    assert (room[:, 0] == 0).all() and (room[:, 1:] == 7.0).all()
