@@ -555,8 +555,9 @@ __global__ __launch_bounds__(256) void k_route_back(RouteArgs a) {
 #pragma unroll
         // (a row of nothing but minus infinity has no scores, and no gradient)
         for (int i = 0; i < N; ++i) d[i] = all != 0.0f ? -d[i] / sum * all : 0.0f;
+        const int named = has ? (int)index : -1;  // (32 bits of another index may name an expert)
         for (int j = 0; j < a.top; ++j) {
-            const int at = __shfl((int)index, first + j) - e0;
+            const int at = __shfl(named, first + j) - e0;
             const float add = __shfl(term, first + j);
 #pragma unroll
             for (int i = 0; i < N; ++i) d[i] += at == i ? add : 0.0f;
