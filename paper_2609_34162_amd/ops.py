@@ -105,7 +105,20 @@ def _packer(kind):
     """A function of a structure's fields, in their order, to its bytes: several times as fast as the
     structure itself, and taken like it where a pointer to one is wanted.  Pointers are numbers."""
     codes = {ctypes.c_int32: "i", ctypes.c_int64: "q", ctypes.c_double: "d", ctypes.c_void_p: "P"}
-    return struct.Struct("@" + "".join(codes.get(t, "P") for _, t in kind._fields_) + "0q").pack
+    codes = [codes.get(t, "P") for _, t in kind._fields_]
+    whole = struct.Struct("@" + "".join(codes) + "0q").pack
+
+    def pack(*values):
+        try:
+            return whole(*values)
+        except (struct.error, OverflowError):
+            for (name, _), code, v in zip(kind._fields_, codes, values):
+                try:
+                    struct.pack(code, v)
+                except (struct.error, OverflowError) as e:
+                    raise ValueError(f"{name}: {e}") from None
+            raise
+    return pack
 
 
 _rows_bytes, _embed_bytes, _norm_bytes, _grads_bytes, _route_bytes, _order_bytes, _expert_bytes = map(
