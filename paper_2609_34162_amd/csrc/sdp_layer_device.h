@@ -127,8 +127,7 @@ __device__ __forceinline__ float lanes_sum(float v, int lanes) {
     return v;
 }
 
-
-// The largest value of such a run, and the smallest.
+// The largest value of such a run.
 __device__ __forceinline__ float lanes_max(float v, int lanes) {
     v = fmaxf(v, lanes_of<0xb1>(v));
     v = fmaxf(v, lanes_of<0x4e>(v));
@@ -136,28 +135,6 @@ __device__ __forceinline__ float lanes_max(float v, int lanes) {
     if (lanes > 8) v = fmaxf(v, lanes_of<0x140>(v));
     if (lanes > 16) v = fmaxf(v, __shfl_xor(v, 16));
     if (lanes > 32) v = fmaxf(v, __shfl_xor(v, 32));
-    return v;
-}
-template <int CONTROL>
-__device__ __forceinline__ int lanes_of_int(int v) {
-    return __builtin_amdgcn_update_dpp(0, v, CONTROL, 0xf, 0xf, true);
-}
-__device__ __forceinline__ int lanes_max_int(int v, int lanes) {
-    v = max(v, lanes_of_int<0xb1>(v));
-    v = max(v, lanes_of_int<0x4e>(v));
-    v = max(v, lanes_of_int<0x141>(v));
-    if (lanes > 8) v = max(v, lanes_of_int<0x140>(v));
-    if (lanes > 16) v = max(v, __shfl_xor(v, 16));
-    if (lanes > 32) v = max(v, __shfl_xor(v, 32));
-    return v;
-}
-__device__ __forceinline__ int lanes_min(int v, int lanes) {
-    v = min(v, lanes_of_int<0xb1>(v));
-    v = min(v, lanes_of_int<0x4e>(v));
-    v = min(v, lanes_of_int<0x141>(v));
-    if (lanes > 8) v = min(v, lanes_of_int<0x140>(v));
-    if (lanes > 16) v = min(v, __shfl_xor(v, 16));
-    if (lanes > 32) v = min(v, __shfl_xor(v, 32));
     return v;
 }
 
