@@ -21,6 +21,10 @@ namespace {
 
 constexpr float kNegInf = -__builtin_huge_valf();
 constexpr int64_t kNotThere = INT64_MIN;
+// Sigmoids that add up to less than this are exp(z) to FP32's last place; their ratios are
+// then taken from the logits, as those of a softmax always are, since the scores may be
+// below any number.
+constexpr float kSmall = 0x1p-26f;
 
 // Larger keys for larger values, the largest for a NaN; -0 counts as 0.
 __device__ __forceinline__ int64_t order_key(double x) {
@@ -55,6 +59,12 @@ __device__ __forceinline__ void put_weight(const RouteArgs &a, int64_t at, float
         store1((uint16_t *)a.weights + at, w);
     else
         ((float *)a.weights)[at] = w;
+}
+
+// 1 / (1 + exp(-x)) by a power that is never past FP32, so that small ones are not lost.
+__device__ __forceinline__ float sigmoid_of(float x) {
+    const float e = expf(-fabsf(x));
+    return (x < 0.0f ? e : 1.0f) / (1.0f + e);
 }
 
 // The largest and the sum of exp(z - max) of a row; max is 0 in a row of nothing but
@@ -153,16 +163,15 @@ __device__ void route_token(const RouteArgs &a, int64_t t, double *value, int64_
     const float x = has ? load1(z + mine) : kNegInf;
     float w;
     if (a.sigmoid)
-        w = has ? 1.0f / (1.0f + expf(-x)) : 0.0f;
+        w = has ? sigmoid_of(x) : 0.0f;
     else
         w = has ? expf(x - top) / sum : 0.0f;
     if (a.renormalize) {
         const float all = wave_sum(w);
-        if (all < 1e-30f) {
-            // too small for their ratios: a sigmoid that far down is exp(z) too
+        if (!a.sigmoid || all < kSmall) {
             const float best = wave_max(x);
             const float e = has ? expf(x - best) : 0.0f, es = wave_sum(e);
-            w = has ? e / es : 0.0f;
+            w = !has ? 0.0f : sum == sum ? e / es : sum;  // (no score of a row with a NaN is a number)
         } else {
             w = has ? w / all : 0.0f;
         }
@@ -466,14 +475,13 @@ __global__ __launch_bounds__(256) void k_route_lanes(RouteArgs a) {
     has = has && sub < a.top;
     float weight;
     if (a.sigmoid)
-        weight = has ? 1.0f / (1.0f + expf(-x)) : 0.0f;
+        weight = has ? sigmoid_of(x) : 0.0f;
     else
         weight = has && (sums || !a.renormalize) ? expf(x - top) * (1.0f / sum) : 0.0f;
     if (a.renormalize) {
         float all = 0.0f;
         if (a.sigmoid) all = lanes_sum(weight, G);
-        if (!a.sigmoid || all < 1e-30f) {
-            // their ratios alone, which scores may be too small for: a sigmoid that far down is exp(z) too
+        if (!a.sigmoid || all < kSmall) {
             const float best = most_of(has ? x : kNegInf);
             weight = has ? expf(x - best) : 0.0f;
             all = lanes_sum(weight, G);
@@ -533,15 +541,14 @@ __global__ __launch_bounds__(256) void k_route_back(RouteArgs a) {
         const bool has = index >= 0 && index < E;
         const float x = has ? load1(row + index) : kNegInf;
         float p = 0.0f;
-        if (has && a.sigmoid) p = 1.0f / (1.0f + expf(-x));
+        if (has && a.sigmoid) p = sigmoid_of(x);
         if (has && all_scores) p = expf(x - top) / sum;
-        const float rest = !has || !a.sigmoid ? 1.0f : 1.0f / (1.0f + expf(x));  // 1 - p
+        const float rest = !has || !a.sigmoid ? 1.0f : sigmoid_of(-x);  // 1 - p
         float term, all = 0.0f;
         if (a.renormalize) {
             const float total = lanes_sum(p, G);
             float q = p / total;
-            if (!a.sigmoid || total < 1e-30f) {
-                // their ratios alone, as forward
+            if (!a.sigmoid || total < kSmall) {
                 const float best = lanes_max(x, G);
                 const float e = has ? expf(x - best) : 0.0f;
                 q = e / lanes_sum(e, G);
@@ -585,7 +592,7 @@ __global__ __launch_bounds__(64) void k_route_back_any(RouteArgs a) {
         const T *z = (const T *)a.logits + t * a.logit_stride;
         T *dz = (T *)a.dlogits + t * a.dlogits_stride;
         float top = 0.0f, sum = 1.0f;
-        if (!a.sigmoid) softmax_of(z, E, top, sum);
+        if (!a.sigmoid && !a.renormalize) softmax_of(z, E, top, sum);
         int64_t index = -1;
         float g = 0.0f;
         if (lane < a.top) {
@@ -595,13 +602,13 @@ __global__ __launch_bounds__(64) void k_route_back_any(RouteArgs a) {
         const bool bad = __any(index >= E);
         const bool has = index >= 0 && index < E;
         const float x = has ? load1(z + index) : kNegInf;
-        const float p = !has ? 0.0f : a.sigmoid ? 1.0f / (1.0f + expf(-x)) : expf(x - top) / sum;
-        const float rest = !has || !a.sigmoid ? 1.0f : 1.0f / (1.0f + expf(x));  // 1 - p
+        const float p = !has ? 0.0f : a.sigmoid ? sigmoid_of(x) : expf(x - top) / sum;
+        const float rest = !has || !a.sigmoid ? 1.0f : sigmoid_of(-x);  // 1 - p
         float term, all = 0.0f;
         if (a.renormalize) {
             float q = p;
             const float total = wave_sum(p);
-            if (total < 1e-30f) {
+            if (!a.sigmoid || total < kSmall) {
                 const float best = wave_max(x);
                 const float e = has ? expf(x - best) : 0.0f;
                 const float es = wave_sum(e);
