@@ -101,18 +101,26 @@ class sdp_expert_desc(ctypes.Structure):
                [("place", ctypes.c_void_p)]
 
 
+def _codes(kind) -> list:
+    codes = {ctypes.c_int32: "i", ctypes.c_int64: "q", ctypes.c_double: "d", ctypes.c_void_p: "P"}
+    return [codes.get(t, "P") for _, t in kind._fields_]
+
+
 def _packer(kind):
     """A function of a structure's fields, in their order, to its bytes: several times as fast as the
     structure itself, and taken like it where a pointer to one is wanted.  Pointers are numbers."""
-    codes = {ctypes.c_int32: "i", ctypes.c_int64: "q", ctypes.c_double: "d", ctypes.c_void_p: "P"}
-    codes = [codes.get(t, "P") for _, t in kind._fields_]
-    whole = struct.Struct("@" + "".join(codes) + "0q").pack
+    return struct.Struct("@" + "".join(_codes(kind)) + "0q").pack
+
+
+def _refusing_packer(kind):
+    """The same where fields are the caller's numbers, one of which may be none that the field holds."""
+    whole = _packer(kind)
 
     def pack(*values):
         try:
             return whole(*values)
         except (struct.error, OverflowError):
-            for (name, _), code, v in zip(kind._fields_, codes, values):
+            for (name, _), code, v in zip(kind._fields_, _codes(kind), values):
                 try:
                     struct.pack(code, v)
                 except (struct.error, OverflowError) as e:
@@ -121,9 +129,10 @@ def _packer(kind):
     return pack
 
 
-_rows_bytes, _embed_bytes, _norm_bytes, _grads_bytes, _route_bytes, _order_bytes, _expert_bytes = map(
-    _packer, (sdp_rows, sdp_embed_desc, sdp_block_norm_desc, sdp_block_norm_grads, sdp_route_desc, sdp_order_desc,
-              sdp_expert_desc))
+_rows_bytes, _grads_bytes, _order_bytes, _expert_bytes = map(
+    _packer, (sdp_rows, sdp_block_norm_grads, sdp_order_desc, sdp_expert_desc))
+_embed_bytes, _norm_bytes, _route_bytes = map(
+    _refusing_packer, (sdp_embed_desc, sdp_block_norm_desc, sdp_route_desc))
 
 
 def _bind():
