@@ -178,10 +178,11 @@ SDP_API int sdp_route(sdp_ctx *ctx, const sdp_route_desc *desc, const void *logi
 
 /* Its backward: dlogits (logit_type, dlogits_stride apart) from the weights'
  * gradient and the index that sdp_route wrote; groups, top_groups and
- * group_best are not looked at.  The choice itself has no gradient.  Negative
- * indexes are places left over; a row with an index past the experts gives
- * NaN.  An index that is named twice counts twice.  dlogits may be logits
- * itself (same stride). */
+ * group_best are not looked at, nor with renormalize logits that the index
+ * does not name.  The choice itself has no gradient.  Negative indexes are
+ * places left over; a row with an index past the experts gives NaN.  An index
+ * that is named twice counts twice.  dlogits may be logits itself (same
+ * stride). */
 SDP_API int sdp_route_backward(sdp_ctx *ctx, const sdp_route_desc *desc, const void *logits, const void *index,
                                const void *dweights, void *dlogits, int64_t dlogits_stride, void *stream);
 

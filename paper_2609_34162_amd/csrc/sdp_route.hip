@@ -231,9 +231,9 @@ __device__ __forceinline__ void sort_list(float *v) {
 // the next one is far enough, and these candidates are ranked by their scores in 64 bits;
 // close groups are compared in 64 bits likewise.  A token that has too many candidates, a
 // NaN or an infinite key is done the slow way, behind the others: one such token makes a
-// call 17 us longer.  Of 32,768 tokens' 256 sigmoid scores with a bias, one in about 100
-// needs the ranking, one in some thousands its groups compared (19.3 us, of which the
-// logits' bytes take 7; without the 64 bits 17.1).
+// call 2 to 5 us longer.  Of 32,768 tokens' 256 sigmoid scores with a bias, one in about
+// 500 needs the ranking, one in about 2,000 its groups compared (18.9 us, of which the
+// logits' bytes take 7; without the 64 bits 16.5).
 // KEEP: how many of its keys a lane's list keeps.  WIDE: a token has 32 or 64 lanes, else
 // 8 or 16.
 template <typename T, int N, int KEEP, bool WIDE, bool SCORED>
@@ -643,7 +643,7 @@ __global__ __launch_bounds__(64) void k_route_back_any(RouteArgs a) {
 
 // Lanes of a token and experts of a lane, 16 where the lanes' lists keep nine of them.
 // The fewest lanes that the experts, the choice and the groups allow: 32,768 tokens of 256
-// experts in groups take 19.3 us with 16 lanes of 16 and 26.7 with 32 of 8.
+// experts in groups take 18.9 us with 16 lanes of 16 and 26.4 with 32 of 8.
 // 0 lanes: none.
 struct Split {
     int lanes, each;
